@@ -13,10 +13,11 @@ Four operators, all reached through `paper_2607_04302_b200.binding`:
 A page holds 64 tokens of every KV head; a head's part has 74 d bytes, groups of 64 values as in include/hifa4.h (along
 d for K, along the page's tokens for V), nibble = 8 + signed code:
   K codes   [64][4][d/64][2] words: units 2p, 2p+1 (8 elements each) of group G at [token][p][G]; element e in nibble e
-  V codes   [d][8] words: word 2i+h holds tokens 16i+4h+(0..3) in nibbles 0..3 and 16i+8+4h+(0..3) in nibbles 4..7
   K shifts  [64][d/64] words: micro-exponent (0..2) of 4-element subgroup 2u+r in bits 16r+2u, +1
+  K scales  [64][d/64] bytes: E6M2 codes
+  V codes   [d][8] words: word 2i+h holds tokens 16i+4h+(0..3) in nibbles 0..3 and 16i+8+4h+(0..3) in nibbles 4..7
   V shifts  [d] words: that of the 4 tokens in nibbles 4r.. of word w in bits 16r+2w, +1
-  K scales  [64][d/64] bytes, V scales [d] bytes: E6M2 codes"""
+  V scales  [d] bytes"""
 import math
 import random
 
@@ -190,9 +191,9 @@ def _pack_v(x):
 
 
 def _regions(d):
-    """Byte offsets of a head's part of a page: K codes, V codes, K shifts, V shifts, K scales, V scales, end."""
+    """Byte offsets of a head's part of a page: codes, shifts and scales of K, then of V."""
     off = [0]
-    for n in (32 * d, 32 * d, 4 * d, 4 * d, d, d):
+    for n in (32 * d, 4 * d, d, 32 * d, 4 * d, d):
         off.append(off[-1] + n)
     return off
 
@@ -201,7 +202,7 @@ def _pack(k, v):
     """[..., 64, d] each -> pages [..., 74 d]."""
     kc, ks, ke = _pack_k(k)
     vc, vs, ve = _pack_v(v)
-    return torch.cat([t.flatten(-2) for t in (kc, vc, ks, vs)] + [ke.flatten(-2), ve], -1)
+    return torch.cat([t.flatten(-2) for t in (kc, ks, ke, vc, vs)] + [ve], -1)
 
 
 def _unpack(pages):
@@ -221,11 +222,11 @@ def _unpack(pages):
 
     lead = pages.shape[:-1]
     kc = codes(part[0]).reshape(lead + (64, 4, G, 2, 8)).movedim(-3, -4).reshape(lead + (64, G, 16, 4))
-    ks = shifts(part[2], [16 * (t % 2) + 2 * (t // 2) for t in range(16)]).reshape(lead + (64, G, 16))
-    ke = S[part[4].reshape(lead + (64, G)).int()]
+    ks = shifts(part[1], [16 * (t % 2) + 2 * (t // 2) for t in range(16)]).reshape(lead + (64, G, 16))
+    ke = S[part[2].reshape(lead + (64, G)).int()]
     K = (kc.float() * ((1 << ks).float() * ke[..., None])[..., None]).reshape(lead + (64, d))
-    vc = codes(part[1]).reshape(lead + (d, 4, 2, 2, 4)).transpose(-2, -3).reshape(lead + (d, 16, 4))
-    vs = shifts(part[3], [16 * r + 2 * (2 * i + h) for i in range(4) for r in range(2) for h in range(2)])
+    vc = codes(part[3]).reshape(lead + (d, 4, 2, 2, 4)).transpose(-2, -3).reshape(lead + (d, 16, 4))
+    vs = shifts(part[4], [16 * r + 2 * (2 * i + h) for i in range(4) for r in range(2) for h in range(2)])
     ve = S[part[5].int()]
     V = (vc.float() * ((1 << vs.reshape(lead + (d, 16))).float() * ve[..., None])[..., None]).reshape(lead + (d, 64))
     return K, V.transpose(-1, -2)
@@ -351,14 +352,14 @@ def _plain_append(st):
         t = torch.arange(head, head + n, device=k.device)
         pg, row = ids[t // 64], t % 64
         rows = st["pages"]
-        for part, lo, width in ((kc, o[0], d // 2), (ks, o[2], 4 * G), (ke, o[4], G)):
+        for part, lo, width in ((kc, o[0], d // 2), (ks, o[1], 4 * G), (ke, o[2], G)):
             view = rows[:, :, lo:lo + 64 * width].unflatten(-1, (64, width))
             view[pg, :, row] = part.transpose(0, 1)
         v = torch.zeros((Hkv, 64 * (p1 - p0), d), device=k.device)
         v[:, :head] = st["v_tail"][b, :, :head].float()
         v[:, head:head + n] = st["v"][b, :, :n].float()
         vc, vs, ve = _pack_v(v.unflatten(1, (p1 - p0, 64)))
-        for part, lo in ((vc, o[1]), (vs, o[3]), (ve[..., None], o[5])):
+        for part, lo in ((vc, o[3]), (vs, o[4]), (ve[..., None], o[5])):
             flat = part.flatten(-2)
             rows[ids, :, lo:lo + flat.shape[-1]] = flat.transpose(0, 1)
         left = end % 64
@@ -531,19 +532,19 @@ def _values_64(pages):
     n, d = pages.shape[0], pages.shape[1] // 74
     G, dev = d // 64, pages.device
     S = torch.tensor(_TABLE64, dtype=torch.float64, device=dev) / 4
-    words = pages[:, :72 * d].contiguous().view(torch.int32).long() & 0xFFFFFFFF
-    scales = pages[:, 72 * d:].long()
-    kw, vw, kx, vx = words[:, :8 * d], words[:, 8 * d:16 * d], words[:, 16 * d:17 * d], words[:, 17 * d:]
+    k_half, v_half = pages[:, :37 * d], pages[:, 37 * d:]
+    kw, vw = (t[:, :36 * d].contiguous().view(torch.int32).long() & 0xFFFFFFFF for t in (k_half, v_half))
+    kw, kx, vw, vx = kw[:, :8 * d], kw[:, 8 * d:], vw[:, :8 * d], vw[:, 8 * d:]
     K = torch.empty((n, 64, d), dtype=torch.float64, device=dev)
     kw, kx = kw.reshape(n, 64, 8 * G), kx.reshape(n, 64, G)
-    ks = S[scales[:, :d].reshape(n, 64, G)]
+    ks = S[k_half[:, 36 * d:].long().reshape(n, 64, G)]
     for c in range(d):
         g, u, e = c // 64, c % 64 // 8, c % 8
         code = (kw[:, :, (u // 2) * 2 * G + 2 * g + u % 2] >> (4 * e)) % 16 - 8
         shift = (kx[:, :, g] >> (2 * u + 16 * (e // 4))) % 4
         K[:, :, c] = code * 2.0 ** shift * ks[:, :, g]
     V = torch.empty((n, 64, d), dtype=torch.float64, device=dev)
-    vw, vs = vw.reshape(n, d, 8), S[scales[:, d:]]
+    vw, vs = vw.reshape(n, d, 8), S[v_half[:, 36 * d:].long()]
     for t in range(64):
         i, r, h, e = t // 16, t // 8 % 2, t // 4 % 2, t % 4
         code = (vw[:, :, 2 * i + h] >> (16 * r + 4 * e)) % 16 - 8
