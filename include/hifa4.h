@@ -326,6 +326,111 @@ int hifa4_attention_fwd_raw(const hifa4_shape* shape, const void* q, const void*
                             void* out, void* workspace, size_t workspace_bytes,
                             int* d_status, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Serving: a paged HIF4 key-value cache, and attention over it.
+ *
+ * A page holds HIFA4_PAGE_TOKENS = 64 consecutive tokens of one sequence, for every KV head: one HIF4 group of V per
+ * channel.  The pool is one buffer of n_pages * Hkv * hifa4_cache_page_bytes(d) bytes, [n_pages][Hkv][74 d] (16-byte
+ * aligned): per value 4 bits of code, 0.5 bits of micro-exponents and 0.125 bits of scale.  Per page and head, in bytes:
+ *   K codes  32 d  [64][4][d/64][2] words: units 2p and 2p+1 (8 elements each) of group G of a token at [token][p][G];
+ *                  element e of the unit in nibble e, nibble = 8 + signed code (value = code * S/4 * 2^shift)
+ *   K shifts  4 d  [64][d/64] words: the shift (0..2) of the 4-element subgroup 2u+r in bits 16r+2u and 16r+2u+1
+ *   K scales    d  [64][d/64] bytes: E6M2 code of S
+ *   V codes  32 d  [d][8] words: word 2i+h has the tokens 16i+4h+(0..3) in nibbles 0..3, 16i+8+4h+(0..3) in nibbles 4..7
+ *   V shifts  4 d  [d] words: the shift of nibbles 4r..4r+3 of word w in bits 16r+2w and 16r+2w+1
+ *   V scales    d  [d] bytes
+ * Scales, shifts and codes are those of hifa4_quantize_qkv (a NaN is stored as zero); tokens behind the end of a sequence
+ * count as zeros in V's groups.  Both halves of the metadata that a lane needs for 8 codes are two bits wide, which is why
+ * the shifts take 32 instead of 24 bits per group.
+ * V's groups run along tokens, so the group of an incomplete page changes with every token.  v_tail keeps the raw values of
+ * the tokens in a sequence's incomplete page, row = position in the page: [n_tails][Hkv][64][d] elements of in_dtype.  It is
+ * read and written by hifa4_cache_append only and may be NULL for the other calls.
+ *
+ * hifa4_seqs: B sequences.  block_table [B][max_pages]: physical page of each logical page; kv_lens [B]: tokens of each
+ * sequence (0 allowed), for hifa4_cache_append including the new ones; tail_slots [B]: a sequence's row of v_tail, NULL: its
+ * index.  All three are DEVICE arrays, so that captured graphs can be replayed with other contents; a length, page or slot
+ * out of range is found on the device: its sequence (a page: its tokens) is left out, and *d_status is set to
+ * HIFA4_ERR_INVALID_ARG.  Block tables of different sequences may share pages for reading; no two sequences of one
+ * hifa4_cache_append may write the same page or tail.
+ *
+ * hifa4_strides: distance in elements between consecutive batch rows, heads and tokens of a 16-bit tensor whose channels are
+ * contiguous; multiples of 8, the tensor 16-byte aligned.  NULL: contiguous [B][H][tokens][d].
+ * ------------------------------------------------------------------------- */
+enum { HIFA4_PAGE_TOKENS = 64 };
+typedef struct {
+    int Hkv, d, in_dtype;
+    int n_pages;
+    void* pages;
+    int n_tails;
+    void* v_tail;
+} hifa4_cache;
+typedef struct {
+    int B, max_pages;
+    const int* block_table;
+    const int* kv_lens;
+    const int* tail_slots;
+} hifa4_seqs;
+typedef struct { long long b, h, t; } hifa4_strides;
+
+/* Bytes of one KV head's part of a page, 74 d; 0 for a d that is not built (64, 128, 256 are). */
+size_t hifa4_cache_page_bytes(int d);
+
+/* Smooth-QK and HIF4 quantization of new tokens into the cache: k, v [B,Hkv,n,d] of cache->in_dtype; sequence b takes its
+ * first n_new[b] tokens (device array; NULL: n of them; 0 allowed) at positions kv_lens[b] - n_new[b] and on.  inv_s: [Hkv,d]
+ * factors of K as in hifa4_quantize_qkv, or NULL.  The incomplete page's older values come from v_tail, so a sequence may be
+ * cut back (kv_lens lowered) inside its last page only, before the next append; nothing else of a page may be appended again. */
+int hifa4_cache_append(const hifa4_cache* cache, const hifa4_seqs* seqs, int n, const int* n_new, const void* k,
+                       const hifa4_strides* k_strides, const void* v, const hifa4_strides* v_strides, const float* inv_s,
+                       int* d_status, void* stream);
+
+/* The values that the cache holds: token i of row b of k_out, v_out [B,Hkv,n,d] (HIFA4_BF16 or HIFA4_F32: both hold every HIF4
+ * value exactly) is the one at position start[b] + i (device array; NULL: 0).  Rows at or behind kv_lens[b] are left as they were. */
+int hifa4_cache_read(const hifa4_cache* cache, const hifa4_seqs* seqs, int n, const int* start, int out_dtype, void* k_out,
+                     void* v_out, int* d_status, void* stream);
+
+/* What the attention calls ask: Hq query heads (q_to_kv as in hifa4_shape: HOST array or NULL), N query tokens per sequence,
+ * causal (hifa4_cache_attention only): query i of a sequence of length L sees the keys up to position L - N + i; otherwise all L.
+ * A query that sees no key gets zeros.  softmax_scale 0 selects 1/sqrt(d). */
+typedef struct {
+    int Hq;
+    const int* q_to_kv;
+    int N, causal, out_dtype;
+    float softmax_scale;
+} hifa4_cache_query;
+
+/* Attention of one new token per sequence over the cache: out [B,Hq,d] = softmax(q~ K^T scale) V on the cache's values, with
+ * q~ = round_in(q * s) (q [B,Hq,d] of cache->in_dtype, q_strides->t unused; s [Hkv,d] or NULL) not quantized: q is a
+ * vanishing part of what a step reads.  Softmax in FP32; P enters the product with V in FP16, scaled to 2^15 at the running maximum.
+ *   lse             [B,Hq] floats or NULL: log(sum_j exp(score_j)), -inf without keys
+ *   page_weight_out [B][max_pages] floats or NULL: page_weight (NULL: zeros; may be the same array) plus the attention weight that
+ *                   the page's tokens got, summed over the query heads.  Entries behind a sequence's last page are left as they were.
+ * query->N must be 1.  workspace: hifa4_cache_decode_workspace_bytes() bytes, 256-byte aligned, its contents irrelevant
+ * before and after; calls that may overlap need one each.  Sums are taken in a fixed order: equal calls give equal bits. */
+size_t hifa4_cache_decode_workspace_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query,
+                                          int with_page_weight);
+int hifa4_cache_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
+                       const hifa4_strides* q_strides, const float* s, void* out, float* lse, const float* page_weight,
+                       float* page_weight_out, void* workspace, size_t workspace_bytes, int* d_status, void* stream);
+
+/* The same for N >= 1 query tokens per sequence: q [B,Hq,N,d], out [B,Hq,N,d].  Cross attention to an encoder's states of other
+ * lengths (causal 0), the next chunk of a prompt or several drafted tokens (causal 1, after their append). */
+size_t hifa4_cache_attention_workspace_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query);
+int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
+                          const hifa4_strides* q_strides, const float* s, void* out, void* workspace, size_t workspace_bytes,
+                          int* d_status, void* stream);
+
+/* Eviction by accumulated attention weight, whole pages (single tokens would break V's groups).  A sequence of more than
+ * keep_pages pages keeps its first keep_first, its last keep_last (>= 1: the incomplete page stays) and, of those between, the
+ * keep_pages - keep_first - keep_last with the largest page_weight (equal weights: the lower index; a NaN counts as less than
+ * everything).  Kept pages close ranks in their order; positions inside K are those of its rotary embedding and stay.
+ *   block_table_out, page_weight_out [B][max_pages], kv_lens_out [B]: may be the inputs themselves; entries behind the last
+ *                   page become -1 and 0;
+ *   freed [B][max_pages], n_freed [B]: physical pages that left the table, in order, -1 behind the last.
+ * seqs->tail_slots is not used.  A sequence whose length is out of range keeps all (see above). */
+int hifa4_cache_evict(const hifa4_seqs* seqs, const float* page_weight, int keep_pages, int keep_first, int keep_last,
+                      int* block_table_out, int* kv_lens_out, float* page_weight_out, int* freed, int* n_freed,
+                      int* d_status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

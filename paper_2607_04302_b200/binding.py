@@ -59,6 +59,25 @@ class _MassStats(C.Structure):
     _fields_ = [("hist", C.c_void_p), ("n_bins", C.c_int), ("lo", C.c_double), ("hi", C.c_double)]
 
 
+class _Cache(C.Structure):
+    _fields_ = [("Hkv", C.c_int), ("d", C.c_int), ("in_dtype", C.c_int), ("n_pages", C.c_int), ("pages", C.c_void_p),
+                ("n_tails", C.c_int), ("v_tail", C.c_void_p)]
+
+
+class _Seqs(C.Structure):
+    _fields_ = [("B", C.c_int), ("max_pages", C.c_int), ("block_table", C.c_void_p), ("kv_lens", C.c_void_p),
+                ("tail_slots", C.c_void_p)]
+
+
+class _Strides(C.Structure):
+    _fields_ = [("b", C.c_longlong), ("h", C.c_longlong), ("t", C.c_longlong)]
+
+
+class _CacheQuery(C.Structure):
+    _fields_ = [("Hq", C.c_int), ("q_to_kv", C.POINTER(C.c_int)), ("N", C.c_int), ("causal", C.c_int), ("out_dtype", C.c_int),
+                ("softmax_scale", C.c_float)]
+
+
 _lib = None
 
 
@@ -124,6 +143,23 @@ def lib():
         L.hifa4_attention_fwd_raw.argtypes = [C.POINTER(_Shape), C.c_void_p, C.c_void_p, C.c_void_p,
                                               C.c_void_p, C.c_void_p, C.POINTER(_AttnParams), C.c_void_p,
                                               C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        P, I, V = C.POINTER, C.c_int, C.c_void_p
+        L.hifa4_cache_page_bytes.restype = C.c_size_t
+        L.hifa4_cache_page_bytes.argtypes = [I]
+        L.hifa4_cache_append.restype = I
+        L.hifa4_cache_append.argtypes = [P(_Cache), P(_Seqs), I, V, V, P(_Strides), V, P(_Strides), V, V, V]
+        L.hifa4_cache_read.restype = I
+        L.hifa4_cache_read.argtypes = [P(_Cache), P(_Seqs), I, V, I, V, V, V, V]
+        L.hifa4_cache_decode_workspace_bytes.restype = C.c_size_t
+        L.hifa4_cache_decode_workspace_bytes.argtypes = [P(_Cache), I, I, P(_CacheQuery), I]
+        L.hifa4_cache_decode.restype = I
+        L.hifa4_cache_decode.argtypes = [P(_Cache), P(_Seqs), P(_CacheQuery), V, P(_Strides), V, V, V, V, V, V, C.c_size_t, V, V]
+        L.hifa4_cache_attention_workspace_bytes.restype = C.c_size_t
+        L.hifa4_cache_attention_workspace_bytes.argtypes = [P(_Cache), I, I, P(_CacheQuery)]
+        L.hifa4_cache_attention.restype = I
+        L.hifa4_cache_attention.argtypes = [P(_Cache), P(_Seqs), P(_CacheQuery), V, P(_Strides), V, V, V, C.c_size_t, V, V]
+        L.hifa4_cache_evict.restype = I
+        L.hifa4_cache_evict.argtypes = [P(_Seqs), V, I, I, I, V, V, V, V, V, V, V]
         _lib = L
     return _lib
 
@@ -135,7 +171,9 @@ EXPORTS = ("hifa4_status_string", "hifa4_get_counters", "hifa4_smooth_calibrate"
            "hifa4_quantize_qkv", "hifa4_attention_workspace_bytes", "hifa4_attention_fwd",
            "hifa4_attention_fwd_stats", "hifa4_attention_raw_workspace_bytes", "hifa4_attention_fwd_raw",
            "hifa4_attention_fwd_qraw", "hifa4_f8qk_workspace_bytes", "hifa4_attention_fwd_f8qk",
-           "hifa4_selftest_wait_timeout")
+           "hifa4_selftest_wait_timeout", "hifa4_cache_page_bytes", "hifa4_cache_append", "hifa4_cache_read",
+           "hifa4_cache_decode_workspace_bytes", "hifa4_cache_decode", "hifa4_cache_attention_workspace_bytes",
+           "hifa4_cache_attention", "hifa4_cache_evict")
 
 
 def status_string(status: int) -> str:
@@ -456,4 +494,191 @@ def attention_fwd_raw(q, k, v, s, inv_s, causal: bool, Bc: int = 64, out_dtype=F
                                        C.byref(prm), _ptr(out), _ptr(workspace),
                                        workspace.numel(), _ptr(d_status), _stream())
     _check(rc, "hifa4_attention_fwd_raw")
+    return out
+
+
+# ---------------------------------------------------------------- paged HIF4 cache
+PAGE_TOKENS = 64
+
+
+@dataclass
+class PagedCache:
+    """Pages of a HIF4 key-value cache and the raw values of the incomplete ones (layouts: include/hifa4.h).
+    v_tail = None: a cache that is only read."""
+    pages: torch.Tensor                     # uint8 [n_pages, Hkv, 74 d]
+    v_tail: torch.Tensor | None = None      # [n_tails, Hkv, 64, d] of the activation dtype
+
+    def struct(self, in_dtype) -> _Cache:
+        pages, tail = self.pages, self.v_tail
+        assert pages.is_cuda and pages.dtype == torch.uint8 and pages.dim() == 3 and pages.is_contiguous()
+        n_pages, Hkv, nbytes = pages.shape
+        assert nbytes % 74 == 0
+        c = _Cache(Hkv, nbytes // 74, in_dtype, n_pages, pages.data_ptr(), 0, None)
+        if tail is not None:
+            assert tail.is_contiguous() and tuple(tail.shape[1:]) == (Hkv, PAGE_TOKENS, nbytes // 74)
+            c.n_tails, c.v_tail = tail.shape[0], tail.data_ptr()
+        return c
+
+
+def cache_page_bytes(d) -> int:
+    return int(lib().hifa4_cache_page_bytes(int(d)))
+
+
+def alloc_cache(n_pages, Hkv, d, dtype, device, n_tails) -> PagedCache:
+    """Pool of n_pages pages and n_tails tails (one per sequence that grows); dtype: torch.float16 or torch.bfloat16."""
+    nb = cache_page_bytes(d)
+    if nb == 0:
+        raise Hifa4Error(2, "hifa4_cache_page_bytes")
+    return PagedCache(torch.zeros((n_pages, Hkv, nb), dtype=torch.uint8, device=device),
+                      torch.zeros((n_tails, Hkv, PAGE_TOKENS, d), dtype=dtype, device=device))
+
+
+def _ints_ok(t, shape):
+    return t is None or (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == shape)
+
+
+def _seqs(block_table, kv_lens, tail_slots=None) -> _Seqs:
+    B, max_pages = block_table.shape
+    assert _ints_ok(block_table, (B, max_pages)) and _ints_ok(kv_lens, (B,)) and _ints_ok(tail_slots, (B,))
+    return _Seqs(B, max_pages, block_table.data_ptr(), kv_lens.data_ptr(), _ptr(tail_slots))
+
+
+def _strides(t) -> _Strides:
+    """Strides of [B,H,n,d] or [B,H,d]; the channels must be contiguous."""
+    assert t.is_cuda and (t.stride(-1) == 1 or t.shape[-1] == 1)
+    st = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(t.dim() - 1)]
+    return _Strides(st[0], st[1], st[2] if t.dim() == 4 else 0)
+
+
+def _floats_ok(t, shape):
+    return t is None or (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == shape)
+
+
+def cache_append(cache: PagedCache, k, v, block_table, kv_lens, n_new=None, inv_s=None, tail_slots=None, d_status=None):
+    """Smooths and quantizes new keys and values k, v [B,Hkv,n,d] into the cache's pages.  kv_lens [B] counts the new
+    tokens; n_new [B]: how many of the n rows a sequence takes (None: all).  int32 device tensors."""
+    B, Hkv, n, d = k.shape
+    st = cache.struct(_DT[k.dtype])
+    assert v.shape == k.shape and v.dtype == k.dtype and (Hkv, d) == (st.Hkv, st.d) and block_table.shape[0] == B
+    assert cache.v_tail is not None and cache.v_tail.dtype == k.dtype
+    assert _ints_ok(n_new, (B,)) and _floats_ok(inv_s, (Hkv, d))
+    sq, ks, vs = _seqs(block_table, kv_lens, tail_slots), _strides(k), _strides(v)
+    rc = lib().hifa4_cache_append(C.byref(st), C.byref(sq), n, _ptr(n_new), _ptr(k), C.byref(ks), _ptr(v), C.byref(vs),
+                                  _ptr(inv_s), _ptr(d_status), _stream())
+    _check(rc, "hifa4_cache_append")
+
+
+def cache_read(cache: PagedCache, block_table, kv_lens, n, start=None, out_dtype=BF16, out=None, d_status=None):
+    """The values in the cache: (k, v) [B,Hkv,n,d], token i of row b at position start[b] + i (None: i).  Rows at or behind
+    kv_lens[b] are left as they were (out = (k, v): the caller's tensors)."""
+    st = cache.struct(BF16)
+    B = block_table.shape[0]
+    shape = (B, st.Hkv, n, st.d)
+    if out is None:
+        out = [cache.pages.new_empty(shape, dtype=_TORCH_DT[out_dtype]) for _ in range(2)]
+    k, v = out
+    assert k.is_contiguous() and v.is_contiguous() and tuple(k.shape) == shape == tuple(v.shape) and k.dtype == v.dtype
+    assert _ints_ok(start, (B,))
+    sq = _seqs(block_table, kv_lens)
+    rc = lib().hifa4_cache_read(C.byref(st), C.byref(sq), n, _ptr(start), _DT[k.dtype], _ptr(k), _ptr(v), _ptr(d_status), _stream())
+    _check(rc, "hifa4_cache_read")
+    return k, v
+
+
+def _cache_query(st, q, s, N, causal, out, softmax_scale, q_to_kv):
+    """Checks q, s and out against the cache; the query struct and the output tensor."""
+    assert q.shape[-1] == st.d and _floats_ok(s, (st.Hkv, st.d))
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert out.is_cuda and out.is_contiguous() and out.shape == q.shape
+    keep, mp = _map_arr(q_to_kv)
+    prm = _CacheQuery(q.shape[1], mp, N, int(causal), _DT[out.dtype], float(softmax_scale))
+    prm._keep = keep
+    return prm, out
+
+
+def cache_decode_workspace_bytes(cache: PagedCache, B, max_pages, Hq, q_to_kv=None, with_page_weight=False) -> int:
+    keep, mp = _map_arr(q_to_kv)
+    prm = _CacheQuery(Hq, mp, 1, 0, F32, 0.0)
+    return int(lib().hifa4_cache_decode_workspace_bytes(C.byref(cache.struct(BF16)), B, max_pages, C.byref(prm),
+                                                        int(with_page_weight)))
+
+
+def cache_decode(q, cache: PagedCache, block_table, kv_lens, s=None, out=None, lse=None, page_weight=None,
+                 page_weight_out=None, workspace=None, softmax_scale=0.0, q_to_kv=None, d_status=None):
+    """Attention of one new token per sequence, q [B,Hq,d], over the cache -> out [B,Hq,d] (dtype of `out`, or of q).
+    lse [B,Hq], page_weight and page_weight_out [B,max_pages]: float32 device tensors, see include/hifa4.h."""
+    B, Hq, d = q.shape
+    st = cache.struct(_DT[q.dtype])
+    assert block_table.shape[0] == B and _floats_ok(lse, (B, Hq))
+    shape = tuple(block_table.shape)
+    assert _floats_ok(page_weight, shape) and _floats_ok(page_weight_out, shape)
+    prm, out = _cache_query(st, q, s, 1, False, out, softmax_scale, q_to_kv)
+    sq, qs = _seqs(block_table, kv_lens), _strides(q)
+    if workspace is None:
+        need = lib().hifa4_cache_decode_workspace_bytes(C.byref(st), B, sq.max_pages, C.byref(prm), int(page_weight_out is not None))
+        workspace = q.new_empty(int(need), dtype=torch.uint8)
+    rc = lib().hifa4_cache_decode(C.byref(st), C.byref(sq), C.byref(prm), _ptr(q), C.byref(qs), _ptr(s), _ptr(out), _ptr(lse),
+                                  _ptr(page_weight), _ptr(page_weight_out), _ptr(workspace), workspace.numel(),
+                                  _ptr(d_status), _stream())
+    _check(rc, "hifa4_cache_decode")
+    return out
+
+
+def cache_attention_workspace_bytes(cache: PagedCache, B, max_pages, Hq, N, causal=False, q_to_kv=None) -> int:
+    keep, mp = _map_arr(q_to_kv)
+    prm = _CacheQuery(Hq, mp, N, int(causal), F32, 0.0)
+    return int(lib().hifa4_cache_attention_workspace_bytes(C.byref(cache.struct(BF16)), B, max_pages, C.byref(prm)))
+
+
+def cache_attention(q, cache: PagedCache, block_table, kv_lens, causal, s=None, out=None, workspace=None, softmax_scale=0.0,
+                    q_to_kv=None, d_status=None):
+    """Attention of q [B,Hq,N,d] over the cache: all keys of each sequence (cross attention), or, causal, those up to the
+    query's own position when the N queries are the sequence's last N tokens -> out [B,Hq,N,d]."""
+    B, Hq, N, d = q.shape
+    st = cache.struct(_DT[q.dtype])
+    assert block_table.shape[0] == B
+    prm, out = _cache_query(st, q, s, N, causal, out, softmax_scale, q_to_kv)
+    sq, qs = _seqs(block_table, kv_lens), _strides(q)
+    if workspace is None:
+        need = lib().hifa4_cache_attention_workspace_bytes(C.byref(st), B, sq.max_pages, C.byref(prm))
+        workspace = q.new_empty(int(need), dtype=torch.uint8)
+    rc = lib().hifa4_cache_attention(C.byref(st), C.byref(sq), C.byref(prm), _ptr(q), C.byref(qs), _ptr(s), _ptr(out),
+                                     _ptr(workspace), workspace.numel(), _ptr(d_status), _stream())
+    _check(rc, "hifa4_cache_attention")
+    return out
+
+
+@dataclass
+class Evicted:
+    """What cache_evict returns: the shorter tables, lengths and weights, and the pages that left."""
+    block_table: torch.Tensor
+    kv_lens: torch.Tensor
+    page_weight: torch.Tensor
+    freed: torch.Tensor
+    n_freed: torch.Tensor
+
+
+def alloc_evicted(block_table) -> Evicted:
+    B = block_table.shape[0]
+    ints = lambda *shape: torch.empty(shape, dtype=torch.int32, device=block_table.device)
+    return Evicted(ints(*block_table.shape), ints(B), torch.empty(block_table.shape, dtype=torch.float32, device=block_table.device),
+                   ints(*block_table.shape), ints(B))
+
+
+def cache_evict(block_table, kv_lens, page_weight, keep_pages, keep_first=1, keep_last=1, out: Evicted | None = None,
+                d_status=None) -> Evicted:
+    """Takes the pages with the least weight out of the block tables of sequences longer than keep_pages pages; the first
+    keep_first and the last keep_last stay.  The tensors of `out` may be the inputs."""
+    shape = tuple(block_table.shape)
+    assert page_weight is not None and _floats_ok(page_weight, shape)
+    sq = _seqs(block_table, kv_lens)
+    if out is None:
+        out = alloc_evicted(block_table)
+    assert _ints_ok(out.block_table, shape) and _ints_ok(out.kv_lens, shape[:1]) and _floats_ok(out.page_weight, shape)
+    assert _ints_ok(out.freed, shape) and _ints_ok(out.n_freed, shape[:1])
+    rc = lib().hifa4_cache_evict(C.byref(sq), _ptr(page_weight), int(keep_pages), int(keep_first), int(keep_last),
+                                 _ptr(out.block_table), _ptr(out.kv_lens), _ptr(out.page_weight), _ptr(out.freed),
+                                 _ptr(out.n_freed), _ptr(d_status), _stream())
+    _check(rc, "hifa4_cache_evict")
     return out

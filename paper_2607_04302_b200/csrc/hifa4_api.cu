@@ -11,8 +11,9 @@ namespace hifa4 {
 static std::atomic<unsigned long long> g_calls[4];
 
 void count_launch() { g_calls[3].fetch_add(1, std::memory_order_relaxed); }
+void count_call(int which) { g_calls[which].fetch_add(1, std::memory_order_relaxed); }
 
-static int check_arch()
+int check_arch()
 {
     int dev = 0, major = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return HIFA4_ERR_CUDA;
@@ -21,7 +22,7 @@ static int check_arch()
     return major == 10 ? HIFA4_OK : HIFA4_ERR_ARCH;
 }
 
-static int build_map(int Hq, int Hkv, const int* q_to_kv, HeadMap& qmap, HeadMap& kmap)
+int build_map(int Hq, int Hkv, const int* q_to_kv, HeadMap& qmap, HeadMap& kmap)
 {
     if (Hq <= 0 || Hkv <= 0 || Hq > HIFA4_MAX_HEADS || Hkv > HIFA4_MAX_HEADS) return HIFA4_ERR_INVALID_ARG;
     if (!q_to_kv && Hq % Hkv) return HIFA4_ERR_INVALID_ARG;

@@ -1,0 +1,84 @@
+// What the kernels of the paged HIF4 cache share: layout of a page, checks of lengths and page numbers, arguments.
+#pragma once
+#include "hifa4_internal.h"
+#include "hifa4_device.cuh"
+
+namespace hifa4 {
+
+// Byte offsets in a head's part of a page (see include/hifa4.h).
+template <int D> struct Page {
+    static constexpr int NG = D / 64;                          // groups per token of K
+    static constexpr int K_CODES = 0, K_SHIFTS = 32 * D, K_SCALES = 36 * D;
+    static constexpr int HALF = 37 * D;                        // V's half repeats the layout of K's
+    static constexpr int BYTES = 74 * D;
+};
+
+struct CacheView {
+    uint8_t* pages;                    // [n_pages][Hkv][74 d]
+    uint16_t* v_tail;                  // [n_tails][Hkv][64][d] or null
+    int n_pages, n_tails, Hkv;
+    int B, max_pages;
+    const int *table, *lens, *slots;
+    int* d_status;
+    // Tokens of sequence b; -1 where the length is out of range.
+    __device__ __forceinline__ int len(int b) const
+    {
+        const int n = __ldg(lens + b);
+        return n < 0 || n > (long long)max_pages * 64 ? -1 : n;
+    }
+    // Pages of sequence b (none where the length is out of range).
+    __device__ __forceinline__ int n_pages_of(int b) const { return (max(len(b), 0) + 63) >> 6; }
+    // Physical page, -1 where it is out of range.
+    __device__ __forceinline__ int page(int b, int p) const
+    {
+        const int g = __ldg(table + (long long)b * max_pages + p);
+        return g < 0 || g >= n_pages ? -1 : g;
+    }
+    __device__ __forceinline__ void invalid() const
+    {
+        if (d_status) *d_status = HIFA4_ERR_INVALID_ARG;
+    }
+};
+
+// A quarter of the scale with E6M2 code c: code * S/4 * 2^shift is the value.
+__device__ __forceinline__ float quarter_scale(uint32_t c) { return __uint_as_float((c << 21) + (77u << 23)); }
+
+struct Strides { long long b, h, t; };
+
+// Query heads sorted by KV head; unit u = (KV head, rows of a block).  A row is (query head, query token).
+struct CacheUnits {
+    uint8_t head[HIFA4_MAX_HEADS];     // query heads in the order of their KV heads
+    short first[HIFA4_MAX_HEADS + 1];  // first entry of `head` of each KV head
+};
+
+struct DecodeArgs {
+    CacheView cache;
+    CacheUnits units;
+    const void* q;
+    Strides qs;
+    const float* s;                    // [Hkv,d] or null
+    int Hq, N, causal, out_dtype;
+    int blocks;                        // row blocks per KV head
+    float scale_log2;                  // softmax scale times log2(e)
+    void* out;                         // [B,Hq,N,d]
+    float* lse;                        // [B,Hq] or null
+    const float* weight;
+    float* weight_out;                 // [B][max_pages] or null
+    float* part_o;                     // partial sums of segments that cross CTAs: [2 * DECODE_CTAS][rows][d]
+    float2* part_ml;                   // their references and sums of p: [2 * DECODE_CTAS][rows]
+    float2* final_ml;                  // the same of whole rows, [B][Hq] (page weights only)
+    float2* page_ml;                   // the same of pages, [B][Hq][max_pages] (page weights only)
+};
+
+cudaError_t launch_cache_append(int dtype, int d, const CacheView& c, int n, const int* n_new, const void* k, Strides ks,
+                                const void* v, Strides vs, const float* inv_s, cudaStream_t st);
+cudaError_t launch_cache_read(int d, const CacheView& c, int n, const int* start, int out_dtype, void* k, void* v,
+                              cudaStream_t st);
+cudaError_t launch_cache_evict(const CacheView& c, const float* weight, int keep, int first, int last, int* table_out,
+                               int* lens_out, float* weight_out, int* freed, int* n_freed, cudaStream_t st);
+constexpr int DECODE_CTAS = 148;       // one per SM; part of the workspace's size
+// Rows per block for a problem with `rows` rows per KV head at most.
+int decode_block_rows(int d, int rows);
+cudaError_t launch_cache_decode(int dtype, int d, int block_rows, const DecodeArgs& a, cudaStream_t st);
+
+}  // namespace hifa4

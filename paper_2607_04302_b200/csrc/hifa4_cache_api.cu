@@ -1,0 +1,231 @@
+// C-ABI entry points of the paged HIF4 cache: argument validation, size queries and launches.
+#include <cmath>
+#include <cstring>
+
+#include "hifa4_cache.cuh"
+
+using namespace hifa4;
+
+namespace {
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+bool built(int d) { return d == 64 || d == 128 || d == 256; }
+
+int check_cache(const hifa4_cache* c, bool write)
+{
+    if (!c || !c->pages || c->n_pages <= 0 || c->Hkv <= 0 || c->Hkv > HIFA4_MAX_HEADS) return HIFA4_ERR_INVALID_ARG;
+    if (c->in_dtype != HIFA4_F16 && c->in_dtype != HIFA4_BF16) return HIFA4_ERR_INVALID_ARG;
+    if (!built(c->d)) return HIFA4_ERR_UNSUPPORTED;
+    if ((uintptr_t)c->pages & 15) return HIFA4_ERR_INVALID_ARG;
+    if (write && (!c->v_tail || c->n_tails <= 0 || ((uintptr_t)c->v_tail & 15))) return HIFA4_ERR_INVALID_ARG;
+    return HIFA4_OK;
+}
+
+int check_seqs(const hifa4_seqs* s, int Hkv)
+{
+    if (!s || s->B <= 0 || s->max_pages <= 0 || !s->block_table || !s->kv_lens) return HIFA4_ERR_INVALID_ARG;
+    if ((long long)s->B * Hkv > 65535 || s->max_pages > (1 << 24)) return HIFA4_ERR_UNSUPPORTED;
+    return HIFA4_OK;
+}
+
+// A 16-bit tensor [B][H][n][d]: its strides, null where it cannot be read with 16-byte loads.
+int check_tensor(const void* p, const hifa4_strides* st, int H, int n, int d, Strides* out)
+{
+    if (!p || ((uintptr_t)p & 15)) return HIFA4_ERR_INVALID_ARG;
+    *out = st ? Strides{st->b, st->h, st->t} : Strides{(long long)H * n * d, (long long)n * d, d};
+    if ((out->b | out->h | out->t) & 7) return HIFA4_ERR_INVALID_ARG;
+    return HIFA4_OK;
+}
+
+CacheView view(const hifa4_cache* c, const hifa4_seqs* s, int* d_status)
+{
+    CacheView v;
+    std::memset(&v, 0, sizeof(v));
+    if (c) {
+        v.pages = (uint8_t*)c->pages;
+        v.v_tail = (uint16_t*)c->v_tail;
+        v.n_pages = c->n_pages;
+        v.n_tails = c->n_tails;
+        v.Hkv = c->Hkv;
+    }
+    v.B = s->B;
+    v.max_pages = s->max_pages;
+    v.table = s->block_table;
+    v.lens = s->kv_lens;
+    v.slots = s->tail_slots;
+    v.d_status = d_status;
+    return v;
+}
+
+int check_query(const hifa4_cache* c, const hifa4_cache_query* q, CacheUnits* units, int* rows)
+{
+    if (!q || q->N <= 0) return HIFA4_ERR_INVALID_ARG;
+    if (q->out_dtype < HIFA4_F16 || q->out_dtype > HIFA4_F32) return HIFA4_ERR_INVALID_ARG;
+    if (q->softmax_scale < 0.f || !std::isfinite(q->softmax_scale)) return HIFA4_ERR_INVALID_ARG;
+    if (q->causal != 0 && q->causal != 1) return HIFA4_ERR_INVALID_ARG;
+    if (q->N > (1 << 20)) return HIFA4_ERR_UNSUPPORTED;
+    HeadMap qmap, kmap;
+    const int rc = build_map(q->Hq, c->Hkv, q->q_to_kv, qmap, kmap);
+    if (rc) return rc;
+    int at = 0, most = 0;
+    for (int g = 0; g < c->Hkv; ++g) {
+        units->first[g] = (short)at;
+        for (int h = 0; h < q->Hq; ++h)
+            if (qmap.kv_of[h] == g) units->head[at++] = (uint8_t)h;
+        most = at - units->first[g] > most ? at - units->first[g] : most;
+    }
+    units->first[c->Hkv] = (short)at;
+    *rows = most * q->N;
+    return HIFA4_OK;
+}
+
+struct DecodeLayout {
+    int block_rows;
+    long long blocks;
+    size_t part_o, part_ml, final_ml, page_ml, total;
+    DecodeLayout(const hifa4_cache* c, int B, int max_pages, const hifa4_cache_query* q, int rows, bool weight)
+    {
+        block_rows = decode_block_rows(c->d, rows);
+        blocks = (rows + block_rows - 1) / block_rows;
+        part_o = 0;
+        size_t off = align256((size_t)2 * DECODE_CTAS * block_rows * c->d * sizeof(float));
+        part_ml = off;
+        off += align256((size_t)2 * DECODE_CTAS * block_rows * sizeof(float2));
+        final_ml = off;
+        if (weight) off += align256((size_t)B * q->Hq * sizeof(float2));
+        page_ml = off;
+        if (weight) off += align256((size_t)B * q->Hq * max_pages * sizeof(float2));
+        total = off;
+    }
+};
+
+int attend(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
+           const hifa4_strides* q_strides, const float* s, void* out, float* lse, const float* weight, float* weight_out,
+           void* workspace, size_t workspace_bytes, int* d_status, void* stream)
+{
+    count_call(2);
+    int rc = check_cache(cache, false);
+    if (rc) return rc;
+    if ((rc = check_seqs(seqs, cache->Hkv))) return rc;
+    DecodeArgs a;
+    std::memset(&a, 0, sizeof(a));
+    int rows;
+    if ((rc = check_query(cache, query, &a.units, &rows))) return rc;
+    if (!out || (weight && !weight_out)) return HIFA4_ERR_INVALID_ARG;
+    if ((rc = check_tensor(q, q_strides, query->Hq, query->N, cache->d, &a.qs))) return rc;
+    const DecodeLayout lay(cache, seqs->B, seqs->max_pages, query, rows, weight_out != nullptr);
+    if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;
+    if ((long long)seqs->B * cache->Hkv * lay.blocks > 0x7FFFFFFFll) return HIFA4_ERR_UNSUPPORTED;
+    if ((rc = check_arch())) return rc;
+    char* ws = (char*)workspace;
+    a.cache = view(cache, seqs, d_status);
+    a.q = q;
+    a.s = s;
+    a.Hq = query->Hq;
+    a.N = query->N;
+    a.causal = query->causal;
+    a.out_dtype = query->out_dtype;
+    a.blocks = (int)lay.blocks;
+    const double scale = query->softmax_scale > 0.f ? query->softmax_scale : 1.0 / std::sqrt((double)cache->d);
+    a.scale_log2 = (float)(scale * 1.4426950408889634);
+    a.out = out;
+    a.lse = lse;
+    a.weight = weight;
+    a.weight_out = weight_out;
+    a.part_o = (float*)(ws + lay.part_o);
+    a.part_ml = (float2*)(ws + lay.part_ml);
+    a.final_ml = weight_out ? (float2*)(ws + lay.final_ml) : nullptr;
+    a.page_ml = weight_out ? (float2*)(ws + lay.page_ml) : nullptr;
+    return launch_cache_decode(cache->in_dtype, cache->d, lay.block_rows, a, (cudaStream_t)stream) == cudaSuccess ? HIFA4_OK
+                                                                                                                  : HIFA4_ERR_CUDA;
+}
+
+size_t attend_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query, bool weight)
+{
+    CacheUnits units;
+    int rows;
+    if (!cache || cache->Hkv <= 0 || cache->Hkv > HIFA4_MAX_HEADS || !built(cache->d) || B <= 0 || max_pages <= 0) return 0;
+    if (check_query(cache, query, &units, &rows)) return 0;
+    return DecodeLayout(cache, B, max_pages, query, rows, weight).total;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hifa4_cache_page_bytes(int d) { return built(d) ? (size_t)74 * d : 0; }
+
+int hifa4_cache_append(const hifa4_cache* cache, const hifa4_seqs* seqs, int n, const int* n_new, const void* k,
+                       const hifa4_strides* k_strides, const void* v, const hifa4_strides* v_strides, const float* inv_s,
+                       int* d_status, void* stream)
+{
+    count_call(1);
+    int rc = check_cache(cache, true);
+    if (rc) return rc;
+    if ((rc = check_seqs(seqs, cache->Hkv))) return rc;
+    if (n <= 0) return HIFA4_ERR_INVALID_ARG;
+    Strides ks, vs;
+    if ((rc = check_tensor(k, k_strides, cache->Hkv, n, cache->d, &ks))) return rc;
+    if ((rc = check_tensor(v, v_strides, cache->Hkv, n, cache->d, &vs))) return rc;
+    if ((rc = check_arch())) return rc;
+    return launch_cache_append(cache->in_dtype, cache->d, view(cache, seqs, d_status), n, n_new, k, ks, v, vs, inv_s,
+                               (cudaStream_t)stream) == cudaSuccess ? HIFA4_OK : HIFA4_ERR_CUDA;
+}
+
+int hifa4_cache_read(const hifa4_cache* cache, const hifa4_seqs* seqs, int n, const int* start, int out_dtype, void* k_out,
+                     void* v_out, int* d_status, void* stream)
+{
+    int rc = check_cache(cache, false);
+    if (rc) return rc;
+    if ((rc = check_seqs(seqs, cache->Hkv))) return rc;
+    if (n <= 0 || !k_out || !v_out) return HIFA4_ERR_INVALID_ARG;
+    if (out_dtype < HIFA4_F16 || out_dtype > HIFA4_F32) return HIFA4_ERR_INVALID_ARG;
+    if (out_dtype == HIFA4_F16) return HIFA4_ERR_UNSUPPORTED;        // does not hold every HIF4 value
+    if ((rc = check_arch())) return rc;
+    return launch_cache_read(cache->d, view(cache, seqs, d_status), n, start, out_dtype, k_out, v_out, (cudaStream_t)stream) ==
+                   cudaSuccess ? HIFA4_OK : HIFA4_ERR_CUDA;
+}
+
+size_t hifa4_cache_decode_workspace_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query,
+                                          int with_page_weight)
+{
+    return query && query->N == 1 ? attend_bytes(cache, B, max_pages, query, with_page_weight != 0) : 0;
+}
+
+int hifa4_cache_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
+                       const hifa4_strides* q_strides, const float* s, void* out, float* lse, const float* page_weight,
+                       float* page_weight_out, void* workspace, size_t workspace_bytes, int* d_status, void* stream)
+{
+    if (!query || query->N != 1) return HIFA4_ERR_INVALID_ARG;
+    return attend(cache, seqs, query, q, q_strides, s, out, lse, page_weight, page_weight_out, workspace, workspace_bytes,
+                  d_status, stream);
+}
+
+size_t hifa4_cache_attention_workspace_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query)
+{
+    return attend_bytes(cache, B, max_pages, query, false);
+}
+
+int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
+                          const hifa4_strides* q_strides, const float* s, void* out, void* workspace, size_t workspace_bytes,
+                          int* d_status, void* stream)
+{
+    return attend(cache, seqs, query, q, q_strides, s, out, nullptr, nullptr, nullptr, workspace, workspace_bytes, d_status, stream);
+}
+
+int hifa4_cache_evict(const hifa4_seqs* seqs, const float* page_weight, int keep_pages, int keep_first, int keep_last,
+                      int* block_table_out, int* kv_lens_out, float* page_weight_out, int* freed, int* n_freed,
+                      int* d_status, void* stream)
+{
+    int rc = check_seqs(seqs, 1);
+    if (rc) return rc;
+    if (!page_weight || !block_table_out || !kv_lens_out || !page_weight_out || !freed || !n_freed) return HIFA4_ERR_INVALID_ARG;
+    if (keep_first < 0 || keep_last < 1 || keep_pages < 0 || (long long)keep_first + keep_last > keep_pages) return HIFA4_ERR_INVALID_ARG;
+    if ((rc = check_arch())) return rc;
+    return launch_cache_evict(view(nullptr, seqs, d_status), page_weight, keep_pages, keep_first, keep_last, block_table_out,
+                              kv_lens_out, page_weight_out, freed, n_freed, (cudaStream_t)stream) == cudaSuccess ? HIFA4_OK
+                                                                                                                 : HIFA4_ERR_CUDA;
+}
+
+}  // extern "C"

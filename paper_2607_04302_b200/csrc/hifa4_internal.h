@@ -10,6 +10,10 @@ namespace hifa4 {
 struct HeadMap;
 
 void count_launch();
+void count_call(int which);             // 0 calibrate, 1 quantize, 2 attention (hifa4_get_counters)
+int check_arch();                       // HIFA4_OK where the current device is of compute capability 10.x
+// Head maps of the query heads and of the KV heads; checks the numbers of heads and the map.
+int build_map(int Hq, int Hkv, const int* q_to_kv, HeadMap& qmap, HeadMap& kmap);
 
 // cudaFuncSetAttribute(MaxDynamicSharedMemorySize) holds for one device only: each launcher keeps one of
 // these per kernel instantiation and opts in once per device, under a lock (host threads may race).
@@ -34,10 +38,10 @@ struct SmemOptIn {
 // Launch that may become resident while its predecessor in the stream drains (programmatic stream serialization): the
 // kernel executes griddepcontrol.wait before it touches memory.
 template <typename... KArgs, typename... Args>
-cudaError_t launch_dependent(void (*kern)(KArgs...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, Args... args)
+cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, Args... args)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
