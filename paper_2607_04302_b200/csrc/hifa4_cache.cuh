@@ -59,11 +59,13 @@ struct DecodeArgs {
     const float* s;                    // [Hkv,d] or null
     int Hq, N, causal, out_dtype;
     int blocks;                        // row blocks per KV head
+    uint32_t one;                      // 1, as a value that the compiler does not know
     float scale_log2;                  // softmax scale times log2(e)
     void* out;                         // [B,Hq,N,d]
     float* lse;                        // [B,Hq] or null
     const float* weight;
     float* weight_out;                 // [B][max_pages] or null
+    float* first;                      // first pieces of warps that go on to other segments: [DECODE_CTAS * warps][rows (d + 2)]
     float* part_o;                     // partial sums of segments that cross CTAs: [2 * DECODE_CTAS][rows][d]
     float2* part_ml;                   // their references and sums of p: [2 * DECODE_CTAS][rows]
     float2* final_ml;                  // the same of whole rows, [B][Hq] (page weights only)
@@ -79,6 +81,7 @@ cudaError_t launch_cache_evict(const CacheView& c, const float* weight, int keep
 constexpr int DECODE_CTAS = 148;       // one per SM; part of the workspace's size
 // Rows per block for a problem with `rows` rows per KV head at most.
 int decode_block_rows(int d, int rows);
+size_t decode_first_floats(int d, int block_rows);
 cudaError_t launch_cache_decode(int dtype, int d, int block_rows, const DecodeArgs& a, cudaStream_t st);
 
 }  // namespace hifa4

@@ -83,13 +83,15 @@ int check_query(const hifa4_cache* c, const hifa4_cache_query* q, CacheUnits* un
 struct DecodeLayout {
     int block_rows;
     long long blocks;
-    size_t part_o, part_ml, final_ml, page_ml, total;
+    size_t first, part_o, part_ml, final_ml, page_ml, total;
     DecodeLayout(const hifa4_cache* c, int B, int max_pages, const hifa4_cache_query* q, int rows, bool weight)
     {
         block_rows = decode_block_rows(c->d, rows);
         blocks = (rows + block_rows - 1) / block_rows;
-        part_o = 0;
-        size_t off = align256((size_t)2 * DECODE_CTAS * block_rows * c->d * sizeof(float));
+        first = 0;
+        size_t off = align256(decode_first_floats(c->d, block_rows) * sizeof(float));
+        part_o = off;
+        off += align256((size_t)2 * DECODE_CTAS * block_rows * c->d * sizeof(float));
         part_ml = off;
         off += align256((size_t)2 * DECODE_CTAS * block_rows * sizeof(float2));
         final_ml = off;
@@ -117,6 +119,7 @@ int attend(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_q
     const DecodeLayout lay(cache, seqs->B, seqs->max_pages, query, rows, weight_out != nullptr);
     if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;
     if ((long long)seqs->B * cache->Hkv * lay.blocks > 0x7FFFFFFFll) return HIFA4_ERR_UNSUPPORTED;
+    if (weight_out && (long long)seqs->B * ((seqs->max_pages + 63) / 64) > 0x7FFFF000ll) return HIFA4_ERR_UNSUPPORTED;
     if ((rc = check_arch())) return rc;
     char* ws = (char*)workspace;
     a.cache = view(cache, seqs, d_status);
@@ -129,10 +132,12 @@ int attend(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_q
     a.blocks = (int)lay.blocks;
     const double scale = query->softmax_scale > 0.f ? query->softmax_scale : 1.0 / std::sqrt((double)cache->d);
     a.scale_log2 = (float)(scale * 1.4426950408889634);
+    a.one = 1;
     a.out = out;
     a.lse = lse;
     a.weight = weight;
     a.weight_out = weight_out;
+    a.first = (float*)(ws + lay.first);
     a.part_o = (float*)(ws + lay.part_o);
     a.part_ml = (float2*)(ws + lay.part_ml);
     a.final_ml = weight_out ? (float2*)(ws + lay.final_ml) : nullptr;
