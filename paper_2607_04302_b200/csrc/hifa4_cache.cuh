@@ -72,6 +72,21 @@ struct DecodeArgs {
     float2* page_ml;                   // the same of pages, [B][Hq][max_pages] (page weights only)
 };
 
+struct TileArgs {
+    CacheView cache;
+    CacheUnits units;
+    const void* q;
+    Strides qs;
+    const float* s;
+    int Hq, N, causal, out_dtype;
+    int items;                         // row blocks per KV head
+    int splits;
+    float scale_log2;
+    void* out;
+    float* part_o;                     // [(sequence, KV head, item, tile), split][128][d] (splits > 1)
+    float2* part_ml;
+};
+
 cudaError_t launch_cache_append(int dtype, int d, const CacheView& c, int n, const int* n_new, const void* k, Strides ks,
                                 const void* v, Strides vs, const float* inv_s, cudaStream_t st);
 cudaError_t launch_cache_read(int d, const CacheView& c, int n, const int* start, int out_dtype, void* k, void* v,
@@ -83,5 +98,9 @@ constexpr int DECODE_CTAS = 148;       // one per SM; part of the workspace's si
 int decode_block_rows(int d, int rows);
 size_t decode_first_floats(int d, int block_rows);
 cudaError_t launch_cache_decode(int dtype, int d, int block_rows, const DecodeArgs& a, cudaStream_t st);
+
+// Query rows that a CTA of the tensor-memory kernel takes.
+int attention_tile_rows(int dtype, int d);
+cudaError_t launch_cache_attention(int dtype, int d, const TileArgs& a, cudaStream_t st);
 
 }  // namespace hifa4

@@ -102,26 +102,11 @@ struct DecodeLayout {
     }
 };
 
-int attend(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
-           const hifa4_strides* q_strides, const float* s, void* out, float* lse, const float* weight, float* weight_out,
-           void* workspace, size_t workspace_bytes, int* d_status, void* stream)
+// Fills what both kernels' arguments have in common.
+template <class Args>
+void common_args(Args& a, const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q, const float* s,
+                 void* out, int* d_status)
 {
-    count_call(2);
-    int rc = check_cache(cache, false);
-    if (rc) return rc;
-    if ((rc = check_seqs(seqs, cache->Hkv))) return rc;
-    DecodeArgs a;
-    std::memset(&a, 0, sizeof(a));
-    int rows;
-    if ((rc = check_query(cache, query, &a.units, &rows))) return rc;
-    if (!out || (weight && !weight_out)) return HIFA4_ERR_INVALID_ARG;
-    if ((rc = check_tensor(q, q_strides, query->Hq, query->N, cache->d, &a.qs))) return rc;
-    const DecodeLayout lay(cache, seqs->B, seqs->max_pages, query, rows, weight_out != nullptr);
-    if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;
-    if ((long long)seqs->B * cache->Hkv * lay.blocks > 0x7FFFFFFFll) return HIFA4_ERR_UNSUPPORTED;
-    if (weight_out && (long long)seqs->B * ((seqs->max_pages + 63) / 64) > 0x7FFFF000ll) return HIFA4_ERR_UNSUPPORTED;
-    if ((rc = check_arch())) return rc;
-    char* ws = (char*)workspace;
     a.cache = view(cache, seqs, d_status);
     a.q = q;
     a.s = s;
@@ -129,11 +114,40 @@ int attend(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_q
     a.N = query->N;
     a.causal = query->causal;
     a.out_dtype = query->out_dtype;
-    a.blocks = (int)lay.blocks;
     const double scale = query->softmax_scale > 0.f ? query->softmax_scale : 1.0 / std::sqrt((double)cache->d);
     a.scale_log2 = (float)(scale * 1.4426950408889634);
-    a.one = 1;
     a.out = out;
+}
+
+int check_call(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
+               const hifa4_strides* q_strides, const void* out, CacheUnits* units, int* rows, Strides* qs)
+{
+    int rc = check_cache(cache, false);
+    if (rc) return rc;
+    if ((rc = check_seqs(seqs, cache->Hkv))) return rc;
+    if ((rc = check_query(cache, query, units, rows))) return rc;
+    if (!out || ((uintptr_t)out & 15)) return HIFA4_ERR_INVALID_ARG;
+    return check_tensor(q, q_strides, query->Hq, query->N, cache->d, qs);
+}
+
+int run_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const CacheUnits& units, int rows,
+               Strides qs, const void* q, const float* s, void* out, float* lse, const float* weight, float* weight_out,
+               void* workspace, size_t workspace_bytes, int* d_status, void* stream)
+{
+    const DecodeLayout lay(cache, seqs->B, seqs->max_pages, query, rows, weight_out != nullptr);
+    if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;
+    if ((long long)seqs->B * cache->Hkv * lay.blocks > 0x7FFFFFFFll) return HIFA4_ERR_UNSUPPORTED;
+    if (weight_out && (long long)seqs->B * ((seqs->max_pages + 63) / 64) > 0x7FFFF000ll) return HIFA4_ERR_UNSUPPORTED;
+    const int rc = check_arch();
+    if (rc) return rc;
+    DecodeArgs a;
+    std::memset(&a, 0, sizeof(a));
+    common_args(a, cache, seqs, query, q, s, out, d_status);
+    char* ws = (char*)workspace;
+    a.units = units;
+    a.qs = qs;
+    a.blocks = (int)lay.blocks;
+    a.one = 1;
     a.lse = lse;
     a.weight = weight;
     a.weight_out = weight_out;
@@ -146,12 +160,38 @@ int attend(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_q
                                                                                                                   : HIFA4_ERR_CUDA;
 }
 
-size_t attend_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query, bool weight)
+// The tensor-memory kernel's grid and workspace.
+struct TileLayout {
+    long long items, blocks;
+    int splits;
+    size_t part_ml, total;
+    TileLayout(const hifa4_cache* c, int B, int max_pages, int rows)
+    {
+        const int block = attention_tile_rows(c->in_dtype, c->d);
+        items = (rows + block - 1) / block;
+        blocks = (long long)B * c->Hkv * items;
+        splits = 1;
+        if (blocks < DECODE_CTAS) splits = (int)(DECODE_CTAS / blocks);
+        const int most = max_pages / 8 > 1 ? max_pages / 8 : 1;
+        if (splits > most) splits = most;
+        part_ml = splits > 1 ? align256((size_t)blocks * block * splits * c->d * sizeof(float)) : 0;
+        total = splits > 1 ? part_ml + align256((size_t)blocks * block * splits * sizeof(float2)) : 0;
+    }
+};
+
+bool tile_kernel_faster(int rows) { return rows > 32; }
+
+// Workspace of a call; 0 where it is not built.
+size_t attend_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query, bool weight, bool many)
 {
     CacheUnits units;
     int rows;
     if (!cache || cache->Hkv <= 0 || cache->Hkv > HIFA4_MAX_HEADS || !built(cache->d) || B <= 0 || max_pages <= 0) return 0;
     if (check_query(cache, query, &units, &rows)) return 0;
+    if (many && tile_kernel_faster(rows)) {
+        const size_t n = TileLayout(cache, B, max_pages, rows).total;
+        return n ? n : 256;
+    }
     return DecodeLayout(cache, B, max_pages, query, rows, weight).total;
 }
 
@@ -195,28 +235,55 @@ int hifa4_cache_read(const hifa4_cache* cache, const hifa4_seqs* seqs, int n, co
 size_t hifa4_cache_decode_workspace_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query,
                                           int with_page_weight)
 {
-    return query && query->N == 1 ? attend_bytes(cache, B, max_pages, query, with_page_weight != 0) : 0;
+    return query && query->N == 1 ? attend_bytes(cache, B, max_pages, query, with_page_weight != 0, false) : 0;
 }
 
 int hifa4_cache_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
                        const hifa4_strides* q_strides, const float* s, void* out, float* lse, const float* page_weight,
                        float* page_weight_out, void* workspace, size_t workspace_bytes, int* d_status, void* stream)
 {
-    if (!query || query->N != 1) return HIFA4_ERR_INVALID_ARG;
-    return attend(cache, seqs, query, q, q_strides, s, out, lse, page_weight, page_weight_out, workspace, workspace_bytes,
-                  d_status, stream);
+    count_call(2);
+    if (!query || query->N != 1 || (page_weight && !page_weight_out)) return HIFA4_ERR_INVALID_ARG;
+    CacheUnits units;
+    int rows;
+    Strides qs;
+    const int rc = check_call(cache, seqs, query, q, q_strides, out, &units, &rows, &qs);
+    if (rc) return rc;
+    return run_decode(cache, seqs, query, units, rows, qs, q, s, out, lse, page_weight, page_weight_out, workspace, workspace_bytes,
+                      d_status, stream);
 }
 
 size_t hifa4_cache_attention_workspace_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query)
 {
-    return attend_bytes(cache, B, max_pages, query, false);
+    return attend_bytes(cache, B, max_pages, query, false, true);
 }
 
 int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
                           const hifa4_strides* q_strides, const float* s, void* out, void* workspace, size_t workspace_bytes,
                           int* d_status, void* stream)
 {
-    return attend(cache, seqs, query, q, q_strides, s, out, nullptr, nullptr, nullptr, workspace, workspace_bytes, d_status, stream);
+    count_call(2);
+    CacheUnits units;
+    int rows;
+    Strides qs;
+    int rc = check_call(cache, seqs, query, q, q_strides, out, &units, &rows, &qs);
+    if (rc) return rc;
+    if (!tile_kernel_faster(rows))
+        return run_decode(cache, seqs, query, units, rows, qs, q, s, out, nullptr, nullptr, nullptr, workspace, workspace_bytes, d_status, stream);
+    const TileLayout lay(cache, seqs->B, seqs->max_pages, rows);
+    if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;
+    if (lay.blocks * lay.splits * 32 > 0x7FFFFFFFll) return HIFA4_ERR_UNSUPPORTED;
+    if ((rc = check_arch())) return rc;
+    TileArgs a;
+    std::memset(&a, 0, sizeof(a));
+    common_args(a, cache, seqs, query, q, s, out, d_status);
+    a.units = units;
+    a.qs = qs;
+    a.items = (int)lay.items;
+    a.splits = lay.splits;
+    a.part_o = (float*)workspace;
+    a.part_ml = (float2*)((char*)workspace + lay.part_ml);
+    return launch_cache_attention(cache->in_dtype, cache->d, a, (cudaStream_t)stream) == cudaSuccess ? HIFA4_OK : HIFA4_ERR_CUDA;
 }
 
 int hifa4_cache_evict(const hifa4_seqs* seqs, const float* page_weight, int keep_pages, int keep_first, int keep_last,
