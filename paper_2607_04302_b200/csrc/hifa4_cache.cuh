@@ -40,8 +40,26 @@ struct CacheView {
     }
 };
 
-// A quarter of the scale with E6M2 code c: code * S/4 * 2^shift is the value.
-__device__ __forceinline__ float quarter_scale(uint32_t c) { return __uint_as_float((c << 21) + (77u << 23)); }
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t c)
+{
+    uint32_t r;                        // (from the operators the compiler forms twice as many instructions)
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(mask), "r"(c));
+    return r;
+}
+// The scale S of code c as a BF16 number in both halves.
+__device__ __forceinline__ uint32_t scale_pair(uint32_t c) { return ((c << 5) + (79u << 7)) * 0x10001u; }
+// A group's shift word, turned so that the shifts of unit u (bits 2 u and 16 + 2 u) come to lie in bits 7-8 and 23-24.
+__device__ __forceinline__ uint32_t shifts_of_unit(uint32_t w, int u) { return __funnelshift_l(w, w, 7 - 2 * u); }
+// One word of codes -> 8 BF16 values, pairs (nibble i, nibble i + 4).  y: see shifts_of_unit; s2: see scale_pair.
+// big = 32 * 2^shift; with a nibble in the mantissa (34 + code / 4) * 2^shift; times S less 34 * 2^shift * S (7 significant bits): exact.
+__device__ __forceinline__ void hif4_word_values(uint32_t w, uint32_t y, uint32_t s2, uint32_t (&r)[4])
+{
+    const uint32_t big = and_or(y, 0x01800180u, 0x42004200u);
+    uint32_t sub = and_or(y, 0x01800180u, 0xC208C208u);                     // -34 * 2^shift
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(sub) : "r"(sub), "r"(s2));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = bf2_fma(and_or(w >> (4 * i), 0x000F000Fu, big), s2, sub);
+}
 
 struct Strides { long long b, h, t; };
 

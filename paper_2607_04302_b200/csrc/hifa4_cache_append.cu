@@ -3,29 +3,55 @@
 
 namespace hifa4 {
 
-// Packed nibbles 8 + m of four biased quotients (hif4_unit: the low byte of bits(y) is the signed code m).
+// Nibbles 8 + m of four biased quotients (hif4_unit: the low byte of bits(y) is the signed code m): elements 0, 1 in byte 0,
+// elements 2, 3 in byte 2.
 __device__ __forceinline__ uint32_t nibbles4(const float* y)
 {
-    uint32_t w = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w |= ((__float_as_uint(y[e]) + 8u) & 15u) << (4 * e);
-    return w;
+    const uint32_t b01 = __byte_perm(__float_as_uint(y[0]), __float_as_uint(y[1]), 0x0040);
+    const uint32_t b23 = __byte_perm(__float_as_uint(y[2]), __float_as_uint(y[3]), 0x0040);
+    const uint32_t n = (__byte_perm(b01, b23, 0x5410) & 0x0F0F0F0Fu) ^ 0x08080808u;       // m + 8 modulo 16
+    return n | (n >> 4);
 }
 
-// One unit (8 elements) of a group: clamps what lies above the E6M2 range, drops NaN, and returns codes and shifts.
-__device__ __forceinline__ void quantize_unit(float (&x)[8], const Hif4Group& g, float (&y)[8], int& k0, int& k1)
+// Largest magnitude of a lane's 16 values (packed pairs), of its group of four lanes; a NaN loses.
+template <typename T> __device__ __forceinline__ float group_max(const uint32_t (&x)[8])
+{
+    uint32_t m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = max16<T>(abs16<T>(x[i]), abs16<T>(x[i + 4]));
+    m[0] = max16<T>(max16<T>(m[0], m[1]), max16<T>(m[2], m[3]));
+    m[0] = max16<T>(m[0], __shfl_xor_sync(0xffffffffu, m[0], 1));
+    m[0] = max16<T>(m[0], __shfl_xor_sync(0xffffffffu, m[0], 2));
+    float a, b;
+    Pair16<T>::unpack(m[0], a, b);
+    return fmaxf(fmaxf(a, b), 0.f);                                          // (a NaN against a NaN)
+}
+
+// A lane's 16 consecutive values (two units) of a group whose largest magnitude is A: nibbles of the four subgroups (nibbles4) and
+// their shifts.  What lies above the E6M2 range saturates, a NaN becomes zero.
+template <typename T>
+__device__ __forceinline__ void quantize16(const uint32_t (&xw)[8], float A, const Hif4Group& g, uint32_t (&nib)[4], int (&k)[4])
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = x[i] > g.top ? g.top : x[i] < -g.top ? -g.top : x[i] == x[i] ? x[i] : 0.f;
-    const float a0 = fmaxf(max3(fabsf(x[0]), fabsf(x[1]), fabsf(x[2])), fabsf(x[3]));
-    const float a1 = fmaxf(max3(fabsf(x[4]), fabsf(x[5]), fabsf(x[6])), fabsf(x[7]));
-    uint32_t w[4];
-    int a;
-    hif4_unit(x, a0, a1, g, w, y, a, k0, k1);
+    for (int u = 0; u < 2; ++u) {
+        float x[8], y[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) Pair16<T>::unpack(xw[4 * u + i], x[2 * i], x[2 * i + 1]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -g.top), g.top) : 0.f;
+        const float a0 = fmaxf(max3(fabsf(x[0]), fabsf(x[1]), fabsf(x[2])), fabsf(x[3]));
+        const float a1 = fmaxf(max3(fabsf(x[4]), fabsf(x[5]), fabsf(x[6])), fabsf(x[7]));
+        uint32_t w[4];
+        int a;
+        hif4_unit(x, a0, a1, g, w, y, a, k[2 * u], k[2 * u + 1]);
+        nib[2 * u] = nibbles4(y);
+        nib[2 * u + 1] = nibbles4(y + 4);
+    }
 }
 
-// One CTA per (sequence, KV head, page that the new tokens touch).  K: a thread per 64-element group of a row.  V: the
-// page's rows, old ones from the tail and new ones, gathered in shared memory; a thread per channel.
+// One CTA per (sequence, KV head, page that the new tokens touch); four lanes per 64-element group, 16 elements each, which
+// are whole words of the page's layout.  K: rows straight from global memory.  V: the page's rows, old ones from the tail and new
+// ones, turned in shared memory; a team takes two adjacent channels.
 // The CTA of a sequence's first page is the one that reads the old tail, so it also writes the new one.
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
@@ -33,8 +59,9 @@ cache_append_kernel(const CacheView c, int n, const int* __restrict__ n_new, con
                     const uint16_t* __restrict__ v, Strides vs, const float* __restrict__ inv_s)
 {
     using P = Page<D>;
-    constexpr int NG = P::NG;
-    __shared__ __align__(16) uint16_t rows[64 * D];
+    constexpr int NG = P::NG, CH = D / 8, KT = 64 * NG * 4 / 256, VT = 64 * CH / 256;
+    __shared__ __align__(16) uint4 rows[64 * CH];        // 16-byte chunk i of row r at i ^ (r / 16): the four lanes of a team read
+                                                         // rows 16 apart
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int b = blockIdx.y / c.Hkv, h = blockIdx.y % c.Hkv, tid = threadIdx.x;
@@ -48,107 +75,137 @@ cache_append_kernel(const CacheView c, int n, const int* __restrict__ n_new, con
     const int begin = len - cnt, p = (begin >> 6) + (int)blockIdx.x, last = (len - 1) >> 6;
     if (p > last) return;
     const int page = c.page(b, p);
-    uint16_t* tail = c.v_tail + ((long long)slot * c.Hkv + h) * 64 * D;
+    uint4* tail = reinterpret_cast<uint4*>(c.v_tail + ((long long)slot * c.Hkv + h) * 64 * D);
     const int lo = max(begin - 64 * p, 0), hi = min(len - 64 * p, 64);     // the page's rows [lo, hi) are new
     const uint16_t* kb = k + b * ks.b + h * ks.h + (64ll * p - begin) * ks.t;   // row 0 of the page
     const uint16_t* vb = v + b * vs.b + h * vs.h + (64ll * p - begin) * vs.t;
-    for (int i = tid; i < 64 * (D / 8); i += 256) {
-        const int r = i / (D / 8), ch = i % (D / 8) * 8;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (r < lo) x = *reinterpret_cast<const uint4*>(tail + r * D + ch);
-        else if (r < hi) x = __ldg(reinterpret_cast<const uint4*>(vb + r * vs.t + ch));
-        *reinterpret_cast<uint4*>(rows + r * D + ch) = x;
+    uint4 vx[VT], kx[KT][2];
+#pragma unroll
+    for (int i = 0; i < VT; ++i) {
+        const int r = (i * 256 + tid) / CH, ch = (i * 256 + tid) % CH;
+        vx[i] = make_uint4(0, 0, 0, 0);
+        if (r < lo) vx[i] = tail[r * CH + ch];
+        else if (r < hi) vx[i] = __ldg(reinterpret_cast<const uint4*>(vb + r * vs.t) + ch);
+    }
+    // K: task = (row, group, lane of the team)
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+        const int t = i * 256 + tid, r = t / (4 * NG);
+        kx[i][0] = kx[i][1] = make_uint4(0, 0, 0, 0);
+        if (r >= lo && r < hi) {
+            const uint4* src = reinterpret_cast<const uint4*>(kb + r * ks.t + t % (4 * NG) / 4 * 64 + t % 4 * 16);
+            kx[i][0] = __ldg(src);
+            kx[i][1] = __ldg(src + 1);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < VT; ++i) {
+        const int r = (i * 256 + tid) / CH, ch = (i * 256 + tid) % CH;
+        rows[r * CH + (ch ^ (r >> 4))] = vx[i];
     }
     __syncthreads();
     if (blockIdx.x == 0) {                                                   // rows of the incomplete page that are new
         const int t0 = last == p ? lo : 0, t1 = len & 63;
         const uint16_t* vl = v + b * vs.b + h * vs.h + (64ll * last - begin) * vs.t;
-        for (int i = tid; i < t1 * (D / 8); i += 256) {
-            const int r = i / (D / 8), ch = i % (D / 8) * 8;
-            if (r >= t0) *reinterpret_cast<uint4*>(tail + r * D + ch) = __ldg(reinterpret_cast<const uint4*>(vl + r * vs.t + ch));
-        }
+        for (int i = tid + t0 * CH; i < t1 * CH; i += 256) tail[i] = __ldg(reinterpret_cast<const uint4*>(vl + i / CH * vs.t) + i % CH);
     }
     if (page < 0) {
         if (tid == 0) c.invalid();
         return;
     }
     uint8_t* pg = c.pages + ((long long)page * c.Hkv + h) * P::BYTES;
-    for (int i = tid + lo * NG; i < hi * NG; i += 256) {
-        const int r = i / NG, G = i % NG;
-        const uint4* src = reinterpret_cast<const uint4*>(kb + r * ks.t + 64 * G);
-        uint32_t xw[32];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint4 x = __ldg(src + j);
-            xw[4 * j] = x.x; xw[4 * j + 1] = x.y; xw[4 * j + 2] = x.z; xw[4 * j + 3] = x.w;
-        }
-        float A = 0.f;
+    for (int i = 0; i < KT; ++i) {
+        const int t = i * 256 + tid, r = t / (4 * NG), G = t % (4 * NG) / 4, j = t % 4;
+        const bool in = r >= lo && r < hi;
+        if (!__any_sync(0xffffffffu, in)) continue;
+        uint32_t xw[8] = {kx[i][0].x, kx[i][0].y, kx[i][0].z, kx[i][0].w, kx[i][1].x, kx[i][1].y, kx[i][1].z, kx[i][1].w};
+        if (inv_s) {                                                         // FP32 product, rounded once to the activation dtype
+            const float4* f = reinterpret_cast<const float4*>(inv_s + h * D + 64 * G + 16 * j);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            float x0, x1;
-            Pair16<T>::unpack(xw[j], x0, x1);
-            if (inv_s) {                                                     // FP32 product, rounded once to the activation dtype
-                const float2 f = __ldg(reinterpret_cast<const float2*>(inv_s + h * D + 64 * G) + j);
-                xw[j] = Pair16<T>::round_pack(x0 * f.x, x1 * f.y);
-                Pair16<T>::unpack(xw[j], x0, x1);
+            for (int e = 0; e < 4; ++e) {
+                const float4 fe = __ldg(f + e);
+                float x0, x1;
+                Pair16<T>::unpack(xw[2 * e], x0, x1);
+                xw[2 * e] = Pair16<T>::round_pack(x0 * fe.x, x1 * fe.y);
+                Pair16<T>::unpack(xw[2 * e + 1], x0, x1);
+                xw[2 * e + 1] = Pair16<T>::round_pack(x0 * fe.z, x1 * fe.w);
             }
-            A = max3(A, fabsf(x0), fabsf(x1));
         }
+        const float A = group_max<T>(xw);
         const Hif4Group g = hif4_group(A);
-        uint32_t shifts = 0;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            float x[8], y[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) Pair16<T>::unpack(xw[4 * u + j], x[2 * j], x[2 * j + 1]);
-            int k0, k1;
-            quantize_unit(x, g, y, k0, k1);
-            *reinterpret_cast<uint32_t*>(pg + P::K_CODES + r * (D / 2) + (u / 2) * 8 * NG + G * 8 + (u % 2) * 4) =
-                nibbles4(y) | nibbles4(y + 4) << 16;
-            shifts |= (uint32_t)k0 << (2 * u) | (uint32_t)k1 << (16 + 2 * u);
+        uint32_t nib[4];
+        int sh[4];
+        quantize16<T>(xw, A, g, nib, sh);
+        uint32_t s = (uint32_t)(sh[0] | sh[1] << 16 | sh[2] << 2 | sh[3] << 18) << (4 * j);
+        s |= __shfl_xor_sync(0xffffffffu, s, 1);
+        s |= __shfl_xor_sync(0xffffffffu, s, 2);
+        if (!in) continue;
+        *reinterpret_cast<uint2*>(pg + P::K_CODES + r * (D / 2) + j * 8 * NG + 8 * G) =
+            make_uint2(__byte_perm(nib[0], nib[1], 0x6420), __byte_perm(nib[2], nib[3], 0x6420));
+        if (j == 0) {
+            *reinterpret_cast<uint32_t*>(pg + P::K_SHIFTS + 4 * (r * NG + G)) = s;
+            pg[P::K_SCALES + r * NG + G] = (uint8_t)g.code;
         }
-        *reinterpret_cast<uint32_t*>(pg + P::K_SHIFTS + 4 * i) = shifts;
-        pg[P::K_SCALES + i] = (uint8_t)g.code;
     }
     uint8_t* vp = pg + P::HALF;
-    for (int ch = tid; ch < D; ch += 256) {
-        float A = 0.f;
-#pragma unroll 16
-        for (int t = 0; t < 64; ++t) A = fmaxf(A, fabsf(In16<T>::to_f(rows[t * D + ch])));
-        const Hif4Group g = hif4_group(A);
-        uint32_t shifts = 0;
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(rows);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t w0 = 0, w1 = 0;
+    for (int t = tid; t < D * 2; t += 256) {                                 // task = (pair of channels, lane of the team)
+        const int cp = t / 4, j = t % 4;
+        uint32_t xa[8], xb[8];                                               // channels 2 cp and 2 cp + 1, pairs of tokens
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {                                    // unit r: tokens 16 i + 8 r + (0..7)
-                float x[8], y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = In16<T>::to_f(rows[(16 * i + 8 * r + e) * D + ch]);
-                int k0, k1;
-                quantize_unit(x, g, y, k0, k1);
-                w0 |= nibbles4(y) << (16 * r);
-                w1 |= nibbles4(y + 4) << (16 * r);
-                shifts |= (uint32_t)k0 << (16 * r + 4 * i) | (uint32_t)k1 << (16 * r + 4 * i + 2);
+        for (int e = 0; e < 8; ++e) {
+            uint32_t x0, x1;
+            {
+                const int r = 16 * j + 2 * e;
+                x0 = words[(r * CH + ((cp / 4) ^ j)) * 4 + cp % 4];
+                x1 = words[((r + 1) * CH + ((cp / 4) ^ j)) * 4 + cp % 4];
             }
-            *reinterpret_cast<uint2*>(vp + P::K_CODES + ch * 32 + i * 8) = make_uint2(w0, w1);
+            xa[e] = __byte_perm(x0, x1, 0x5410);
+            xb[e] = __byte_perm(x0, x1, 0x7632);
         }
-        *reinterpret_cast<uint32_t*>(vp + P::K_SHIFTS + 4 * ch) = shifts;
-        vp[P::K_SCALES + ch] = (uint8_t)g.code;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t (&xw)[8] = x ? xb : xa;
+            const float A = group_max<T>(xw);
+            const Hif4Group g = hif4_group(A);
+            uint32_t nib[4];
+            int sh[4];
+            quantize16<T>(xw, A, g, nib, sh);                                // subgroups: tokens 16 j + 4 i + (0..3); word h: i = h and h + 2
+            uint32_t s = (uint32_t)(sh[0] | sh[1] << 2 | sh[2] << 16 | sh[3] << 18) << (4 * j);
+            s |= __shfl_xor_sync(0xffffffffu, s, 1);
+            s |= __shfl_xor_sync(0xffffffffu, s, 2);
+            const int ch = 2 * cp + x;
+            *reinterpret_cast<uint2*>(vp + P::K_CODES + ch * 32 + j * 8) =
+                make_uint2(__byte_perm(nib[0], nib[2], 0x6420), __byte_perm(nib[1], nib[3], 0x6420));
+            if (j == 0) {
+                *reinterpret_cast<uint32_t*>(vp + P::K_SHIFTS + 4 * ch) = s;
+                vp[P::K_SCALES + ch] = (uint8_t)g.code;
+            }
+        }
     }
 }
 
-__device__ __forceinline__ void store_value(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store_value(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }   // exact
+// Eight values of a row from their BF16 pairs.
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const uint32_t (&x)[4]) { *reinterpret_cast<uint4*>(p) = make_uint4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void store8(float* p, const uint32_t (&x)[4])
+{
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(x[0] << 16, x[0] & 0xFFFF0000u, x[1] << 16, x[1] & 0xFFFF0000u);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(x[2] << 16, x[2] & 0xFFFF0000u, x[3] << 16, x[3] & 0xFFFF0000u);
+}
 
-// One CTA per (sequence, KV head, page).  A thread per element: bound by its stores.
+// One CTA per (sequence, KV head, page): the page's codes to shared memory, half of the threads on K, half on V.  K: a thread
+// per unit of a row.  V: a thread per word of eight channels, whose 64 values are turned in registers, so that it stores 16
+// bytes (FP32: 32) of eight rows.
 template <typename O, int D>
 __global__ void __launch_bounds__(256)
 cache_read_kernel(const CacheView c, int n, const int* __restrict__ start, O* __restrict__ k_out, O* __restrict__ v_out)
 {
     using P = Page<D>;
     constexpr int NG = P::NG;
-    __shared__ __align__(16) uint32_t sm[P::BYTES / 4];
+    constexpr int V_AT = P::HALF, V_SHIFTS = V_AT + 36 * D;      // V codes with 32 bytes of padding after every eight channels
+    __shared__ __align__(16) uint8_t sm[V_AT + 41 * D];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int b = blockIdx.y / c.Hkv, h = blockIdx.y % c.Hkv, tid = threadIdx.x;
@@ -166,28 +223,46 @@ cache_read_kernel(const CacheView c, int n, const int* __restrict__ start, O* __
         return;
     }
     const uint4* src = reinterpret_cast<const uint4*>(c.pages + ((long long)page * c.Hkv + h) * P::BYTES);
-    for (int i = tid; i < P::BYTES / 16; i += 256) reinterpret_cast<uint4*>(sm)[i] = __ldg(src + i);
+    for (int i = tid; i < P::BYTES / 16; i += 256) {
+        const int v16 = i - P::HALF / 16;                        // 16-byte piece of V's half
+        const int dst = v16 < 0 ? i : P::HALF / 16 + (v16 < 2 * D ? v16 + v16 / 16 * 2 : v16 + D / 4);
+        reinterpret_cast<uint4*>(sm)[dst] = __ldg(src + i);
+    }
     __syncthreads();
-    const uint8_t* by = reinterpret_cast<const uint8_t*>(sm);
     const int lo = max(begin - 64 * p, 0), hi = min(end - 64 * p, 64);
     const long long row0 = ((long long)b * c.Hkv + h) * n + 64ll * p - begin;
-    for (int i = tid; i < 64 * D; i += 256) {
-        const int r = i / D, ch = i % D;
-        if (r < lo || r >= hi) continue;
-        const long long o = (row0 + r) * D + ch;
-        {
-            const int G = ch / 64, u = ch % 64 / 8, e = ch % 8;
-            const uint32_t w = sm[r * (D / 8) + (u / 2) * 2 * NG + 2 * G + u % 2];
-            const int sh = (sm[P::K_SHIFTS / 4 + r * NG + G] >> (16 * (e / 4) + 2 * u)) & 3;
-            const float s4 = quarter_scale(by[P::K_SCALES + r * NG + G]);
-            store_value(k_out + o, (float)(((int)(w >> (4 * e)) & 15) - 8) * __uint_as_float(__float_as_uint(s4) + (sh << 23)));
+    if (tid < 128) {
+        for (int t = tid; t < 64 * D / 8; t += 128) {
+            const int r = t / (D / 8), u = t % (D / 8), G = u / 8, uu = u % 8;
+            if (r < lo || r >= hi) continue;
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(sm + P::K_CODES + r * (D / 2) + (uu / 2) * 8 * NG + 8 * G + uu % 2 * 4);
+            const uint32_t sh = *reinterpret_cast<const uint32_t*>(sm + P::K_SHIFTS + 4 * (r * NG + G));
+            uint32_t x[4];
+            hif4_word_values(w, shifts_of_unit(sh, uu), scale_pair(sm[P::K_SCALES + r * NG + G]), x);
+            const uint32_t y[4] = {__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410), __byte_perm(x[0], x[1], 0x7632),
+                                   __byte_perm(x[2], x[3], 0x7632)};
+            store8(k_out + (row0 + r) * D + 8 * u, y);
         }
-        {
-            const int w_i = 2 * (r / 16) + r / 4 % 2, hf = r / 8 % 2, e = r % 4;
-            const uint32_t w = sm[P::HALF / 4 + ch * 8 + w_i];
-            const int sh = (sm[(P::HALF + P::K_SHIFTS) / 4 + ch] >> (16 * hf + 2 * w_i)) & 3;
-            const float s4 = quarter_scale(by[P::HALF + P::K_SCALES + ch]);
-            store_value(v_out + o, (float)(((int)(w >> (16 * hf + 4 * e)) & 15) - 8) * __uint_as_float(__float_as_uint(s4) + (sh << 23)));
+        return;
+    }
+    for (int t = tid - 128; t < D; t += 128) {
+        const int w = t % 8, o = t / 8;
+        uint32_t x[8][4];                                        // channel 8 o + i: pairs of tokens 16 (w / 2) + 4 (w % 2) + e, + 8
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int ch = 8 * o + i;
+            const uint32_t code = *reinterpret_cast<const uint32_t*>(sm + V_AT + ch * 32 + o * 32 + w * 4);
+            const uint32_t sh = *reinterpret_cast<const uint32_t*>(sm + V_SHIFTS + 4 * ch);
+            hif4_word_values(code, shifts_of_unit(sh, w), scale_pair(sm[V_SHIFTS + 4 * D + ch]), x[i]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int r = 16 * (w / 2) + 4 * (w % 2) + e % 4 + e / 4 * 8;
+            if (r < lo || r >= hi) continue;
+            const uint32_t sel = e < 4 ? 0x5410 : 0x7632;
+            const uint32_t y[4] = {__byte_perm(x[0][e % 4], x[1][e % 4], sel), __byte_perm(x[2][e % 4], x[3][e % 4], sel),
+                                   __byte_perm(x[4][e % 4], x[5][e % 4], sel), __byte_perm(x[6][e % 4], x[7][e % 4], sel)};
+            store8(v_out + (row0 + r) * D + 8 * o, y);
         }
     }
 }

@@ -57,24 +57,6 @@ __device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity, volatil
     return false;
 }
 
-// One word of codes -> 8 BF16 values, pairs (nibble i, nibble i + 4).  y: shifts in bits 7-8 and 23-24; s2: the scale S in both halves.
-// big = 32 * 2^shift; with a nibble in the mantissa (34 + code / 4) * 2^shift; times S less 34 * 2^shift * S (7 significant bits): exact.
-__device__ __forceinline__ void values8(uint32_t w, uint32_t y, uint32_t s2, uint32_t (&r)[4])
-{
-    uint32_t big, sub;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(big) : "r"(y), "r"(0x01800180u), "r"(0x42004200u));
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(sub) : "r"(y), "r"(0x01800180u), "r"(0xC208C208u));
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(sub) : "r"(sub), "r"(s2));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t x;
-        asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(x) : "r"(w >> (4 * i)), "r"(0x000F000Fu), "r"(big));
-        r[i] = bf2_fma(x, s2, sub);
-    }
-}
-__device__ __forceinline__ uint32_t scale_pair(uint32_t c) { return ((c << 5) + (79u << 7)) * 0x10001u; }
-__device__ __forceinline__ uint32_t turn7(uint32_t w, int p) { return __funnelshift_l(w, w, 7 - 4 * p); }
-
 __device__ __forceinline__ void tile_store(const TileArgs& a, long long i, float x, float y)
 {
     if (a.out_dtype == HIFA4_BF16) ((uint32_t*)a.out)[i / 2] = Pair16<__nv_bfloat16>::round_pack(x, y);
@@ -365,11 +347,11 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
                     asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w0), "=r"(w1) : "r"(raw + P::K_CODES + row * (D / 2) + p * 8 * NG + 8 * G));
                     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sh) : "r"(raw + P::K_SHIFTS + 4 * (row * NG + G)));
                     asm volatile("ld.shared.u8 %0, [%1];" : "=r"(sc) : "r"(raw + P::K_SCALES + row * NG + G));
-                    const uint32_t y = turn7(sh, p), s2 = scale_pair(sc), dst = k_t + G * 8192 + row * 128;
-                    values8(w0, y, s2, o);
+                    const uint32_t y = shifts_of_unit(sh, 2 * p), s2 = scale_pair(sc), dst = k_t + G * 8192 + row * 128;
+                    hif4_word_values(w0, y, s2, o);
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + ((uint32_t)((2 * p) ^ (row & 7)) << 4)), "r"(o[0]), "r"(o[1]),
                                  "r"(o[2]), "r"(o[3]) : "memory");
-                    values8(w1, y >> 2, s2, o);
+                    hif4_word_values(w1, y >> 2, s2, o);
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + ((uint32_t)((2 * p + 1) ^ (row & 7)) << 4)), "r"(o[0]), "r"(o[1]),
                                  "r"(o[2]), "r"(o[3]) : "memory");
                 }
@@ -386,11 +368,11 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
                 asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w0), "=r"(w1) : "r"(raw + P::HALF + P::K_CODES + ch * 32 + p * 8));
                 asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sh) : "r"(raw + P::HALF + P::K_SHIFTS + 4 * ch));
                 asm volatile("ld.shared.u8 %0, [%1];" : "=r"(sc) : "r"(raw + P::HALF + P::K_SCALES + ch));
-                const uint32_t y = turn7(sh, p), s2 = scale_pair(sc), dst = v_t + ch * 128;
-                values8(w0, y, s2, o);
+                const uint32_t y = shifts_of_unit(sh, 2 * p), s2 = scale_pair(sc), dst = v_t + ch * 128;
+                hif4_word_values(w0, y, s2, o);
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + ((uint32_t)((2 * p) ^ (ch & 7)) << 4)), "r"(o[0]), "r"(o[1]),
                              "r"(o[2]), "r"(o[3]) : "memory");
-                values8(w1, y >> 2, s2, o);
+                hif4_word_values(w1, y >> 2, s2, o);
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + ((uint32_t)((2 * p + 1) ^ (ch & 7)) << 4)), "r"(o[0]), "r"(o[1]),
                              "r"(o[2]), "r"(o[3]) : "memory");
             }

@@ -27,12 +27,6 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t c)
-{
-    uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(mask), "r"(c));
-    return r;
-}
 // a + c in the multiply-add pipe (one: 1, which the compiler must not know): the logic pipe, half as wide, is the busier one.
 __device__ __forceinline__ uint32_t add_mad(uint32_t a, uint32_t one, uint32_t c)
 {
@@ -43,7 +37,7 @@ __device__ __forceinline__ uint32_t add_mad(uint32_t a, uint32_t one, uint32_t c
 // Eight codes of a word as four packed pairs (nibble i, nibble i + 4) of code * 2^shift / 2 in FP16.  y holds the two shifts in the
 // low exponent bits (10-11 and 26-27); its other bits do not matter.  A nibble lands in the mantissa of a power of two whose
 // exponent's low two bits are clear, so one logic operation with y forms that number times 2^shift; what the number is too large
-// by is subtracted.  All steps are exact.  (Written as lop3: from the operators the compiler forms twice as many.)
+// by is subtracted.  All steps are exact.
 __device__ __forceinline__ void unpack8(uint32_t w, uint32_t y, uint32_t one, uint32_t (&r)[4])
 {
     const uint32_t big = and_or(y, 0x0C000C00u, 0x60006000u);         // 512 * 2^shift; with a nibble: (512 + nibble / 2) * 2^shift
