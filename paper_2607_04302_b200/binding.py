@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from functools import lru_cache
 
 import torch
 
@@ -501,23 +502,30 @@ def attention_fwd_raw(q, k, v, s, inv_s, causal: bool, Bc: int = 64, out_dtype=F
 PAGE_TOKENS = 64
 
 
-@dataclass
+@dataclass(frozen=True)
 class PagedCache:
     """Pages of a HIF4 key-value cache and the raw values of the incomplete ones (layouts: include/hifa4.h).
     v_tail = None: a cache that is only read."""
     pages: torch.Tensor                     # uint8 [n_pages, Hkv, 74 d]
     v_tail: torch.Tensor | None = None      # [n_tails, Hkv, 64, d] of the activation dtype
 
-    def struct(self, in_dtype) -> _Cache:
+    def __post_init__(self):
         pages, tail = self.pages, self.v_tail
         assert pages.is_cuda and pages.dtype == torch.uint8 and pages.dim() == 3 and pages.is_contiguous()
         n_pages, Hkv, nbytes = pages.shape
         assert nbytes % 74 == 0
-        c = _Cache(Hkv, nbytes // 74, in_dtype, n_pages, pages.data_ptr(), 0, None)
+        n_tails = 0
         if tail is not None:
-            assert tail.is_contiguous() and tuple(tail.shape[1:]) == (Hkv, PAGE_TOKENS, nbytes // 74)
-            c.n_tails, c.v_tail = tail.shape[0], tail.data_ptr()
-        return c
+            assert tail.is_cuda and tail.is_contiguous() and tuple(tail.shape[1:]) == (Hkv, PAGE_TOKENS, nbytes // 74)
+            n_tails = tail.shape[0]
+        # the C descriptors, formed once: a call's host time counts
+        make = lambda dt: _Cache(Hkv, nbytes // 74, dt, n_pages, pages.data_ptr(), n_tails, _ptr(tail))
+        object.__setattr__(self, "_st", {dt: make(dt) for dt in (F16, BF16)})
+
+    def struct(self, in_dtype) -> _Cache:
+        st = self._st[in_dtype]
+        assert st.pages == self.pages.data_ptr() and (self.v_tail is None or st.v_tail == self.v_tail.data_ptr())
+        return st
 
 
 def cache_page_bytes(d) -> int:
@@ -534,24 +542,27 @@ def alloc_cache(n_pages, Hkv, d, dtype, device, n_tails) -> PagedCache:
 
 
 def _ints_ok(t, shape):
-    return t is None or (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == shape)
-
-
-def _seqs(block_table, kv_lens, tail_slots=None) -> _Seqs:
-    B, max_pages = block_table.shape
-    assert _ints_ok(block_table, (B, max_pages)) and _ints_ok(kv_lens, (B,)) and _ints_ok(tail_slots, (B,))
-    return _Seqs(B, max_pages, block_table.data_ptr(), kv_lens.data_ptr(), _ptr(tail_slots))
-
-
-def _strides(t) -> _Strides:
-    """Strides of [B,H,n,d] or [B,H,d]; the channels must be contiguous."""
-    assert t.is_cuda and (t.stride(-1) == 1 or t.shape[-1] == 1)
-    st = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(t.dim() - 1)]
-    return _Strides(st[0], st[1], st[2] if t.dim() == 4 else 0)
+    return t is None or (t.dtype is torch.int32 and t.shape == shape and t.is_cuda and t.is_contiguous())
 
 
 def _floats_ok(t, shape):
-    return t is None or (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == shape)
+    return t is None or (t.dtype is torch.float32 and t.shape == shape and t.is_cuda and t.is_contiguous())
+
+
+def _seqs(block_table, kv_lens, tail_slots=None) -> _Seqs:
+    shape = B, max_pages = block_table.shape
+    assert _ints_ok(block_table, shape) and _ints_ok(kv_lens, shape[:1]) and _ints_ok(tail_slots, shape[:1])
+    return _Seqs(B, max_pages, block_table.data_ptr(), kv_lens.data_ptr(), _ptr(tail_slots))
+
+
+def _strides(t):
+    """Reference to the strides of [B,H,n,d] or [B,H,d] (channels contiguous), None where all is contiguous."""
+    assert t.is_cuda
+    if t.is_contiguous():
+        return None
+    assert t.stride(-1) == 1
+    st = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(t.dim() - 1)]
+    return C.byref(_Strides(st[0], st[1], st[2] if t.dim() == 4 else 0))
 
 
 def cache_append(cache: PagedCache, k, v, block_table, kv_lens, n_new=None, inv_s=None, tail_slots=None, d_status=None):
@@ -559,13 +570,13 @@ def cache_append(cache: PagedCache, k, v, block_table, kv_lens, n_new=None, inv_
     tokens; n_new [B]: how many of the n rows a sequence takes (None: all).  int32 device tensors."""
     B, Hkv, n, d = k.shape
     st = cache.struct(_DT[k.dtype])
-    assert v.shape == k.shape and v.dtype == k.dtype and (Hkv, d) == (st.Hkv, st.d) and block_table.shape[0] == B
-    assert cache.v_tail is not None and cache.v_tail.dtype == k.dtype
+    assert v.shape == k.shape and v.dtype is k.dtype and Hkv == st.Hkv and d == st.d and block_table.shape[0] == B
+    assert cache.v_tail is not None and cache.v_tail.dtype is k.dtype
     assert _ints_ok(n_new, (B,)) and _floats_ok(inv_s, (Hkv, d))
-    sq, ks, vs = _seqs(block_table, kv_lens, tail_slots), _strides(k), _strides(v)
-    rc = lib().hifa4_cache_append(C.byref(st), C.byref(sq), n, _ptr(n_new), _ptr(k), C.byref(ks), _ptr(v), C.byref(vs),
-                                  _ptr(inv_s), _ptr(d_status), _stream())
-    _check(rc, "hifa4_cache_append")
+    rc = lib().hifa4_cache_append(C.byref(st), C.byref(_seqs(block_table, kv_lens, tail_slots)), n, _ptr(n_new), k.data_ptr(),
+                                  _strides(k), v.data_ptr(), _strides(v), _ptr(inv_s), _ptr(d_status), _stream())
+    if rc:
+        _check(rc, "hifa4_cache_append")
 
 
 def cache_read(cache: PagedCache, block_table, kv_lens, n, start=None, out_dtype=BF16, out=None, d_status=None):
@@ -585,23 +596,24 @@ def cache_read(cache: PagedCache, block_table, kv_lens, n, start=None, out_dtype
     return k, v
 
 
-def _cache_query(st, q, s, N, causal, out, softmax_scale, q_to_kv):
-    """Checks q, s and out against the cache; the query struct and the output tensor."""
-    assert q.shape[-1] == st.d and _floats_ok(s, (st.Hkv, st.d))
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    assert out.is_cuda and out.is_contiguous() and out.shape == q.shape
+@lru_cache(maxsize=1024)
+def _cache_workspace_bytes(call, Hkv, d, dtype, B, max_pages, Hq, N, q_to_kv, weight):
+    """Size query of "decode" or "attention" by the sizes alone."""
     keep, mp = _map_arr(q_to_kv)
-    prm = _CacheQuery(q.shape[1], mp, N, int(causal), _DT[out.dtype], float(softmax_scale))
-    prm._keep = keep
-    return prm, out
+    prm = C.byref(_CacheQuery(Hq, mp, N, 0, F32, 0.0))
+    st = C.byref(_Cache(Hkv, d, dtype, 1, None, 0, None))
+    if call == "decode":
+        return int(lib().hifa4_cache_decode_workspace_bytes(st, B, max_pages, prm, int(weight)))
+    return int(lib().hifa4_cache_attention_workspace_bytes(st, B, max_pages, prm))
+
+
+def _tuple(q_to_kv):
+    return None if q_to_kv is None else tuple(int(x) for x in q_to_kv)
 
 
 def cache_decode_workspace_bytes(cache: PagedCache, B, max_pages, Hq, q_to_kv=None, with_page_weight=False) -> int:
-    keep, mp = _map_arr(q_to_kv)
-    prm = _CacheQuery(Hq, mp, 1, 0, F32, 0.0)
-    return int(lib().hifa4_cache_decode_workspace_bytes(C.byref(cache.struct(BF16)), B, max_pages, C.byref(prm),
-                                                        int(with_page_weight)))
+    st = cache.struct(BF16)
+    return _cache_workspace_bytes("decode", st.Hkv, st.d, BF16, B, max_pages, Hq, 1, _tuple(q_to_kv), bool(with_page_weight))
 
 
 def cache_decode(q, cache: PagedCache, block_table, kv_lens, s=None, out=None, lse=None, page_weight=None,
@@ -609,26 +621,30 @@ def cache_decode(q, cache: PagedCache, block_table, kv_lens, s=None, out=None, l
     """Attention of one new token per sequence, q [B,Hq,d], over the cache -> out [B,Hq,d] (dtype of `out`, or of q).
     lse [B,Hq], page_weight and page_weight_out [B,max_pages]: float32 device tensors, see include/hifa4.h."""
     B, Hq, d = q.shape
-    st = cache.struct(_DT[q.dtype])
-    assert block_table.shape[0] == B and _floats_ok(lse, (B, Hq))
-    shape = tuple(block_table.shape)
+    dt = _DT[q.dtype]
+    st, sq = cache.struct(dt), _seqs(block_table, kv_lens)
+    shape = block_table.shape
+    assert d == st.d and B == sq.B and _floats_ok(s, (st.Hkv, d)) and _floats_ok(lse, (B, Hq))
     assert _floats_ok(page_weight, shape) and _floats_ok(page_weight_out, shape)
-    prm, out = _cache_query(st, q, s, 1, False, out, softmax_scale, q_to_kv)
-    sq, qs = _seqs(block_table, kv_lens), _strides(q)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    assert out.is_cuda and out.is_contiguous() and out.shape == q.shape
     if workspace is None:
-        need = lib().hifa4_cache_decode_workspace_bytes(C.byref(st), B, sq.max_pages, C.byref(prm), int(page_weight_out is not None))
-        workspace = q.new_empty(int(need), dtype=torch.uint8)
-    rc = lib().hifa4_cache_decode(C.byref(st), C.byref(sq), C.byref(prm), _ptr(q), C.byref(qs), _ptr(s), _ptr(out), _ptr(lse),
-                                  _ptr(page_weight), _ptr(page_weight_out), _ptr(workspace), workspace.numel(),
-                                  _ptr(d_status), _stream())
-    _check(rc, "hifa4_cache_decode")
+        workspace = q.new_empty(_cache_workspace_bytes("decode", st.Hkv, d, dt, B, sq.max_pages, Hq, 1, _tuple(q_to_kv),
+                                                       page_weight_out is not None), dtype=torch.uint8)
+    keep, mp = _map_arr(q_to_kv)
+    rc = lib().hifa4_cache_decode(C.byref(st), C.byref(sq), C.byref(_CacheQuery(Hq, mp, 1, 0, _DT[out.dtype], softmax_scale)),
+                                  q.data_ptr(), _strides(q), _ptr(s), out.data_ptr(), _ptr(lse), _ptr(page_weight),
+                                  _ptr(page_weight_out), workspace.data_ptr(), workspace.numel(), _ptr(d_status), _stream())
+    if rc:
+        _check(rc, "hifa4_cache_decode")
     return out
 
 
-def cache_attention_workspace_bytes(cache: PagedCache, B, max_pages, Hq, N, causal=False, q_to_kv=None) -> int:
-    keep, mp = _map_arr(q_to_kv)
-    prm = _CacheQuery(Hq, mp, N, int(causal), F32, 0.0)
-    return int(lib().hifa4_cache_attention_workspace_bytes(C.byref(cache.struct(BF16)), B, max_pages, C.byref(prm)))
+def cache_attention_workspace_bytes(cache: PagedCache, B, max_pages, Hq, N, dtype=torch.bfloat16, q_to_kv=None) -> int:
+    dt = _DT[dtype]
+    st = cache.struct(dt)
+    return _cache_workspace_bytes("attention", st.Hkv, st.d, dt, B, max_pages, Hq, N, _tuple(q_to_kv), False)
 
 
 def cache_attention(q, cache: PagedCache, block_table, kv_lens, causal, s=None, out=None, workspace=None, softmax_scale=0.0,
@@ -636,16 +652,21 @@ def cache_attention(q, cache: PagedCache, block_table, kv_lens, causal, s=None, 
     """Attention of q [B,Hq,N,d] over the cache: all keys of each sequence (cross attention), or, causal, those up to the
     query's own position when the N queries are the sequence's last N tokens -> out [B,Hq,N,d]."""
     B, Hq, N, d = q.shape
-    st = cache.struct(_DT[q.dtype])
-    assert block_table.shape[0] == B
-    prm, out = _cache_query(st, q, s, N, causal, out, softmax_scale, q_to_kv)
-    sq, qs = _seqs(block_table, kv_lens), _strides(q)
+    dt = _DT[q.dtype]
+    st, sq = cache.struct(dt), _seqs(block_table, kv_lens)
+    assert d == st.d and B == sq.B and _floats_ok(s, (st.Hkv, d))
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    assert out.is_cuda and out.is_contiguous() and out.shape == q.shape
     if workspace is None:
-        need = lib().hifa4_cache_attention_workspace_bytes(C.byref(st), B, sq.max_pages, C.byref(prm))
-        workspace = q.new_empty(int(need), dtype=torch.uint8)
-    rc = lib().hifa4_cache_attention(C.byref(st), C.byref(sq), C.byref(prm), _ptr(q), C.byref(qs), _ptr(s), _ptr(out),
-                                     _ptr(workspace), workspace.numel(), _ptr(d_status), _stream())
-    _check(rc, "hifa4_cache_attention")
+        workspace = q.new_empty(_cache_workspace_bytes("attention", st.Hkv, d, dt, B, sq.max_pages, Hq, N, _tuple(q_to_kv), False),
+                                dtype=torch.uint8)
+    keep, mp = _map_arr(q_to_kv)
+    rc = lib().hifa4_cache_attention(C.byref(st), C.byref(sq), C.byref(_CacheQuery(Hq, mp, N, causal, _DT[out.dtype], softmax_scale)),
+                                     q.data_ptr(), _strides(q), _ptr(s), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                     _ptr(d_status), _stream())
+    if rc:
+        _check(rc, "hifa4_cache_attention")
     return out
 
 
