@@ -86,6 +86,8 @@ struct DecodeArgs {
     float* first;                      // first pieces of warps that go on to other segments: [DECODE_CTAS * warps][rows (d + 2)]
     float* part_o;                     // partial sums of segments that cross CTAs: [2 * DECODE_CTAS][rows][d]
     float2* part_ml;                   // their references and sums of p: [2 * DECODE_CTAS][rows]
+    int4* begun;                       // [DECODE_CTAS]: sequence, unit and last CTA of the segment that goes on behind a CTA, -1: none
+    int2* seg_ctas;                    // [B][units]: first and last CTA of each segment (page weights only)
     float2* final_ml;                  // the same of whole rows, [B][Hq] (page weights only)
     float2* page_ml;                   // the same of pages, [B][Hq][max_pages] (page weights only)
 };

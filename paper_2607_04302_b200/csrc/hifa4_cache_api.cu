@@ -83,7 +83,7 @@ int check_query(const hifa4_cache* c, const hifa4_cache_query* q, CacheUnits* un
 struct DecodeLayout {
     int block_rows;
     long long blocks;
-    size_t first, part_o, part_ml, final_ml, page_ml, total;
+    size_t first, part_o, part_ml, begun, seg_ctas, final_ml, page_ml, total;
     DecodeLayout(const hifa4_cache* c, int B, int max_pages, const hifa4_cache_query* q, int rows, bool weight)
     {
         block_rows = decode_block_rows(c->d, rows);
@@ -94,6 +94,10 @@ struct DecodeLayout {
         off += align256((size_t)2 * DECODE_CTAS * block_rows * c->d * sizeof(float));
         part_ml = off;
         off += align256((size_t)2 * DECODE_CTAS * block_rows * sizeof(float2));
+        begun = off;
+        off += align256(DECODE_CTAS * sizeof(int4));
+        seg_ctas = off;
+        if (weight) off += align256((size_t)B * c->Hkv * blocks * sizeof(int2));
         final_ml = off;
         if (weight) off += align256((size_t)B * q->Hq * sizeof(float2));
         page_ml = off;
@@ -136,7 +140,7 @@ int run_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cac
 {
     const DecodeLayout lay(cache, seqs->B, seqs->max_pages, query, rows, weight_out != nullptr);
     if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;
-    if ((long long)seqs->B * cache->Hkv * lay.blocks > 0x7FFFFFFFll) return HIFA4_ERR_UNSUPPORTED;
+    if ((2.0 * seqs->max_pages + 1) * seqs->B * cache->Hkv * lay.blocks > 2.0e9) return HIFA4_ERR_UNSUPPORTED;      // steps of work are numbered in 32 bits
     if (weight_out && (long long)seqs->B * ((seqs->max_pages + 63) / 64) > 0x7FFFF000ll) return HIFA4_ERR_UNSUPPORTED;
     const int rc = check_arch();
     if (rc) return rc;
@@ -154,6 +158,8 @@ int run_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cac
     a.first = (float*)(ws + lay.first);
     a.part_o = (float*)(ws + lay.part_o);
     a.part_ml = (float2*)(ws + lay.part_ml);
+    a.begun = (int4*)(ws + lay.begun);
+    a.seg_ctas = weight_out ? (int2*)(ws + lay.seg_ctas) : nullptr;
     a.final_ml = weight_out ? (float2*)(ws + lay.final_ml) : nullptr;
     a.page_ml = weight_out ? (float2*)(ws + lay.page_ml) : nullptr;
     return launch_cache_decode(cache->in_dtype, cache->d, lay.block_rows, a, (cudaStream_t)stream) == cudaSuccess ? HIFA4_OK

@@ -3,7 +3,8 @@
 //   S = q~ K^T scale,  m = running max,  p = exp2(S log2e - m + 15),  l = sum p,  O = p V / l
 //
 // Work: the (sequence, block of query rows of a KV head, page) triples of all sequences, in this order, are dealt out to the
-// consumer warps of one CTA per SM in equal contiguous ranges, whatever the sequences' lengths.  A consumer takes whole pages on
+// consumer warps of one CTA per SM in contiguous ranges of equal cost, whatever the sequences' lengths: a page costs two steps,
+// beginning a (sequence, block) one (400 of 1500 instructions, and what it stores).  A consumer takes whole pages on
 // its own: it forms S of the page's 64 tokens, its softmax and O, all in registers, without any exchange between
 // warps.  One more warp loads the pages (bulk copies, a lane per consumer).  The pages of one (sequence, block) that a
 // range holds are a piece of its segment; pieces that warps of one CTA share are joined in shared memory, those that CTAs share by
@@ -25,6 +26,13 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The same from zero (an operand that is a register set to zero first costs that instruction).
+__device__ __forceinline__ void mma16816_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // a + c in the multiply-add pipe (one: 1, which the compiler must not know): the logic pipe, half as wide, is the busier one.
@@ -105,49 +113,87 @@ struct Cursor {
     int b, u, p, np;
 };
 
-// Pages of sequences [0, upto), times the units per sequence.  Whole block; all threads get the sum.
-__device__ __forceinline__ long long pages_before(const CacheView& c, int upto, long long* scratch)
+// Inclusive prefix sum over a warp.
+__device__ __forceinline__ int warp_scan(int x, int lane)
 {
-    long long s = 0;
-    for (int b = threadIdx.x; b < upto; b += blockDim.x) s += c.n_pages_of(b);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
+
+// Steps of a (sequence, block) of np pages.  Page p is step 2 p + 1; a range of steps has the pages whose steps are in it.
+__device__ __forceinline__ int steps_of(int np) { return np ? 2 * np + 1 : 0; }
+
+// Steps of all sequences, for one block each.  Every warp sums for itself where that takes few loads (no barrier to wait for),
+// else the block does.  All threads of the block call it together and get the sum.
+__device__ __forceinline__ int all_steps(const CacheView& c, int* scratch)
+{
+    int s = 0;
+    if (c.B <= 128) {
+        for (int b = threadIdx.x & 31; b < c.B; b += 32) s += steps_of(c.n_pages_of(b));
+        return __reduce_add_sync(0xffffffffu, s);
+    }
+    for (int b = threadIdx.x; b < c.B; b += blockDim.x) s += steps_of(c.n_pages_of(b));
+    s = __reduce_add_sync(0xffffffffu, s);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = s;
     __syncthreads();
-    long long t = 0;
+    int t = 0;
     for (int w = 0; w < (int)(blockDim.x >> 5); ++w) t += scratch[w];
     return t;
 }
 
-// Where page `at` of the list of work is (at is less than the list's length).  Whole warp.
-__device__ __forceinline__ Cursor locate(const CacheView& c, int U, long long at, int lane)
+// The first page at or behind step `at` of the list of work (at is less than the list's length; np = 0: there is none), its
+// index among all pages and its segment's first step.  Whole warp.
+__device__ __forceinline__ Cursor locate(const CacheView& c, int U, int at, int lane, int* index, int* seg)
 {
-    Cursor cur{0, 0, 0, 1};
-    long long before = 0;
+    Cursor cur{0, 0, 0, 0};
+    int steps = 0, pages = 0;                          // of the sequences before
     for (int b0 = 0; b0 < c.B; b0 += 32) {
-        const int np = b0 + lane < c.B ? c.n_pages_of(b0 + lane) : 0;
-        int pre = np;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, pre, o);
-            if (lane >= o) pre += x;
-        }
-        const unsigned hit = __ballot_sync(0xffffffffu, (before + pre) * U > at);
+        const int np = b0 + lane < c.B ? c.n_pages_of(b0 + lane) : 0, pre = warp_scan(steps_of(np), lane), pre_p = warp_scan(np, lane);
+        const unsigned hit = __ballot_sync(0xffffffffu, (steps + pre) * U > at);
         if (hit) {
             const int l = __ffs(hit) - 1;
             cur.b = b0 + l;
             cur.np = __shfl_sync(0xffffffffu, np, l);
-            before += __shfl_sync(0xffffffffu, pre - np, l);
+            steps += __shfl_sync(0xffffffffu, pre - steps_of(np), l);
+            pages += __shfl_sync(0xffffffffu, pre_p - np, l);
             break;
         }
-        before += __shfl_sync(0xffffffffu, pre, 31);
+        steps += __shfl_sync(0xffffffffu, pre, 31);
+        pages += __shfl_sync(0xffffffffu, pre_p, 31);
     }
-    const int in = (int)(at - before * U);
-    cur.u = in / cur.np;
-    cur.p = in % cur.np;
+    const int in = at - steps * U, size = steps_of(cur.np);
+    cur.u = (int)((unsigned)in / (unsigned)size);
+    cur.p = (in - cur.u * size) >> 1;
+    *seg = steps * U + cur.u * size;
+    *index = pages * U + cur.u * cur.np + cur.p;
+    if (cur.p == cur.np) {                             // the last step of a segment: on to the next one
+        *seg += size;
+        cur.p = 0;
+        if (++cur.u == U) {
+            cur.u = 0;
+            do { ++cur.b; } while (cur.b < c.B && c.n_pages_of(cur.b) == 0);
+            cur.np = cur.b < c.B ? c.n_pages_of(cur.b) : 0;
+        }
+    }
     return cur;
 }
+
+// Equal shares of n things for `parts`: where share i begins, the first n % parts being one longer; and whose thing x is.
+struct Shares {
+    int per, more;
+    __device__ __forceinline__ Shares(int n, int parts) : per((int)((unsigned)n / (unsigned)parts)), more(n - per * parts) {}
+    __device__ __forceinline__ int begin(int i) const { return i * per + min(i, more); }
+    __device__ __forceinline__ int owner(int x) const
+    {
+        const int cut = more * (per + 1);
+        return x < cut ? (int)((unsigned)x / (unsigned)(per + 1)) : more + (int)((unsigned)(x - cut) / (unsigned)per);
+    }
+};
 
 __device__ __forceinline__ float warp_max(float x)
 {
@@ -162,20 +208,23 @@ __device__ __forceinline__ float warp_sum(float x)
     return x;
 }
 
-// CTAs that take part: every one of them has a page at least.
-__device__ __forceinline__ int active_ctas(long long total) { return (int)min((long long)DECODE_CTAS, total); }
+// CTAs that take part: two steps each at least, so that every one that a segment passes through has a page of it.
+__device__ __forceinline__ int active_ctas(int total) { return min(DECODE_CTAS, total / 2); }
 
 __device__ __forceinline__ int units_per_seq(const DecodeArgs& a) { return a.cache.Hkv * a.blocks; }
+
+__device__ __forceinline__ int kv_of(const DecodeArgs& a, int u) { return a.blocks == 1 ? u : (int)((unsigned)u / (unsigned)a.blocks); }
 
 // Row r of unit u: query head and token; false behind the last row.
 template <int ROWS>
 __device__ __forceinline__ bool row_of(const DecodeArgs& a, int u, int r, int& head, int& tok)
 {
-    const int kv = u / a.blocks, i = (u % a.blocks) * ROWS + r;
+    const int kv = kv_of(a, u), i = (u - kv * a.blocks) * ROWS + r;
     const int first = a.units.first[kv], n = (a.units.first[kv + 1] - first) * a.N;
     if (i >= n) return false;
-    head = a.units.head[first + i / a.N];
-    tok = i % a.N;
+    const int h = a.N == 1 ? i : (int)((unsigned)i / (unsigned)a.N);
+    head = a.units.head[first + h];
+    tok = i - h * a.N;
     return true;
 }
 
@@ -192,6 +241,24 @@ __device__ __forceinline__ void store_row_stats(const DecodeArgs& a, int b, int 
     if (a.final_ml) a.final_ml[(long long)b * a.Hq + head] = make_float2(m, l);
 }
 
+// A lane's share of the query rows of a segment, 16 channels of each group of row nt * 8 + g.
+template <int D, int NT> struct QueryLoad {
+    uint4 x[NT][D / 64][2];
+    template <int ROWS> __device__ __forceinline__ void issue(const DecodeArgs& a, const Cursor& cur, int g, int t)
+    {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            int head = 0, tok = 0;
+            const bool have = row_of<ROWS>(a, cur.u, nt * 8 + g, head, tok);
+            const uint4* p = reinterpret_cast<const uint4*>((const uint16_t*)a.q + cur.b * a.qs.b + head * a.qs.h + tok * a.qs.t) + 2 * t;
+#pragma unroll
+            for (int G = 0; G < D / 64; ++G)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) x[nt][G][i] = have ? __ldg(p + 8 * G + i) : make_uint4(0, 0, 0, 0);
+        }
+    }
+};
+
 // Factor that takes sums under the reference m to the reference M >= m (both -inf: nothing there).
 __device__ __forceinline__ float rebase(float m, float M) { return m == -INFINITY ? 0.f : exp2f(m - M); }
 
@@ -204,14 +271,14 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
     constexpr int NG = P::NG, W = C::W, ROWS = C::ROWS;
     constexpr bool BF = sizeof(T) == 2 && !__is_same(T, __half);
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long scratch[W + 1];
-    __shared__ Cursor begin_of[W];                     // first page of a consumer's range
-    __shared__ int pages_of[W];
+    __shared__ int scratch[W + 1];
+    __shared__ Cursor begin_of[W + 1];                 // first page of a consumer's range
+    __shared__ int first_page[W + 1];                  // its index among all pages
     __shared__ volatile int page_there[W];             // whether the page in a consumer's buffers exists
     __shared__ volatile int gave_up;
     __shared__ Cursor piece[2 * W];                    // pieces of segments that a consumer shares with others: [2 w] begun before it,
                                                        // [2 w + 1] in it
-    __shared__ long long piece_at[2 * W];              // index of the segment's first page in the list of work, -1: no such piece
+    __shared__ int piece_at[2 * W];                    // the segment's first step, -1: no such piece
     __shared__ float* piece_of[2 * W];                 // where it is
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -225,35 +292,41 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const CacheView& c = a.cache;
     const int U = units_per_seq(a);
-    const long long total = pages_before(c, c.B, scratch) * U;
-    const int ctas = active_ctas(total);
-    if ((int)blockIdx.x >= ctas) return;
-    const long long cta0 = total * blockIdx.x / ctas, cta1 = total * (blockIdx.x + 1) / ctas;
-    Cursor cur{0, 0, 0, 0};
-    int remaining = 0;
-    long long seg_at = 0;                              // index of the present segment's first page
-    if (warp < W) {
-        const long long nw = (long long)ctas * W, w0 = total * ((long long)blockIdx.x * W + warp) / nw;
-        remaining = (int)(total * ((long long)blockIdx.x * W + warp + 1) / nw - w0);
-        if (remaining > 0) cur = locate(c, U, w0, lane);
-        seg_at = w0 - cur.p;
+    const int total = all_steps(c, scratch) * U, ctas = active_ctas(total);
+    if ((int)blockIdx.x >= ctas) {
+        if (tid == 0) a.begun[blockIdx.x].x = -1;
+        return;
+    }
+    const Shares of_ctas(total, ctas);
+    const int cta0 = of_ctas.begin(blockIdx.x), cta1 = of_ctas.begin(blockIdx.x + 1);
+    Cursor cur;
+    int seg_at;                                        // the present segment's first step
+    QueryLoad<D, NT> ql;
+    {
+        const Shares of_warps(cta1 - cta0, W);
+        const int w0 = cta0 + of_warps.begin(warp);    // warp W: where the next CTA begins
+        int index;
+        cur = locate(c, U, min(w0, total - 1), lane, &index, &seg_at);
+        if (warp < W && cur.np > 0) ql.template issue<ROWS>(a, cur, g, t);      // ahead of the flood of page loads
         if (lane == 0) {
             begin_of[warp] = cur;
-            pages_of[warp] = remaining;
+            first_page[warp] = index;
         }
     }
     __syncthreads();
+    int remaining = warp < W ? first_page[warp + 1] - first_page[warp] : 0;
     if (warp == W) {
         // ---- loads: lane i feeds consumer i, a half page at a time, whenever the consumer has read the one before
         if (lane < W) {
             Cursor ld = begin_of[lane];
-            int halves = 2 * pages_of[lane], i = 0, id = halves ? c.page(ld.b, ld.p) : -1, kv = ld.u / a.blocks;
+            int halves = 2 * (first_page[lane + 1] - first_page[lane]), i = 0, id = halves ? c.page(ld.b, ld.p) : -1, kv = kv_of(a, ld.u);
             const uint32_t dst = smem_u32(smem) + lane * C::PER_WARP, bar = smem_u32(smem) + C::BAR_OFF + 32 * lane;
-            for (uint32_t polls = 0; i < halves && polls < (1u << 22); ++polls) {           // polls since the last load
+            for (uint32_t polls = 0; i < halves && polls < (1u << 20); ++polls) {           // polls since the last load
                 const int half = i & 1;
                 // the first page finds its buffers empty; later ones wait for the reading of the page before
                 if (i >= 2 && !mbar_test_wait(bar + 16 + 8 * half, (uint32_t)(i / 2 - 1) & 1u)) {
                     if ((polls & 63) == 63 && gave_up) break;
+                    __nanosleep(100);                              // half a page takes 2 us: no hurry, and polls take issue slots
                     continue;
                 }
                 if (!half) page_there[lane] = id >= 0;             // read before V's half is released
@@ -272,7 +345,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
                             ld.u = 0;
                             do { ++ld.b; } while ((ld.np = c.n_pages_of(ld.b)) == 0);
                         }
-                        kv = ld.u / a.blocks;
+                        kv = kv_of(a, ld.u);
                     }
                     id = c.page(ld.b, ld.p);
                 }
@@ -285,7 +358,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
 #pragma unroll 1
     while (remaining > 0 && ok) {
         // ---- a segment: query operands
-        const int kv = cur.u / a.blocks, len = c.len(cur.b);
+        const int kv = kv_of(a, cur.u), len = c.len(cur.b);
         float f_log2[NT][2];                           // what makes a product a score times log2(e), columns 2t, 2t + 1
         int stat_row[NT][2];                           // (sequence, query head) of columns 2t, 2t + 1, -1: no such row
         int limit[NT][2];                              // keys that the rows of columns 2t, 2t + 1 see
@@ -293,19 +366,15 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             int head = 0, tok = 0;
-            const bool have = row_of<ROWS>(a, cur.u, nt * 8 + g, head, tok);
-            const uint16_t* qp = (const uint16_t*)a.q + cur.b * a.qs.b + head * a.qs.h + tok * a.qs.t;
             uint32_t x[NG][8];                                      // elements 16t..16t+15 of each group
             float top = 0.f;
 #pragma unroll
             for (int G = 0; G < NG; ++G) {
-                uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-                if (have) {
-                    lo = __ldg(reinterpret_cast<const uint4*>(qp + 64 * G + 16 * t));
-                    hi = __ldg(reinterpret_cast<const uint4*>(qp + 64 * G + 16 * t) + 1);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint4 v = ql.x[nt][G][i];
+                    x[G][4 * i] = v.x; x[G][4 * i + 1] = v.y; x[G][4 * i + 2] = v.z; x[G][4 * i + 3] = v.w;
                 }
-                x[G][0] = lo.x; x[G][1] = lo.y; x[G][2] = lo.z; x[G][3] = lo.w;
-                x[G][4] = hi.x; x[G][5] = hi.y; x[G][6] = hi.z; x[G][7] = hi.w;
                 if (a.s) {                                          // FP32 product, rounded once to the activation dtype
                     const float4* sp = reinterpret_cast<const float4*>(a.s + kv * D + 64 * G + 16 * t);
 #pragma unroll
@@ -423,10 +492,6 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
                     }
                 }
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[i][nt][e] = 0.f;
-#pragma unroll
                 for (int G = 0; G < NG; ++G) {
                     uint32_t A[2][2][4];                              // [row half][unit][step]
 #pragma unroll
@@ -437,14 +502,13 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                        float acc[4];
+                        mma16816_first(acc, A[0][0][0], A[1][0][0], A[0][1][0], A[1][1][0], qf[nt][G][0][0], qf[nt][G][1][0]);
 #pragma unroll
-                        for (int x = 0; x < 4; ++x)
+                        for (int x = 1; x < 4; ++x)
                             mma16816(acc, A[0][0][x], A[1][0][x], A[0][1][x], A[1][1][x], qf[nt][G][0][x], qf[nt][G][1][x]);
-                        s[i][nt][0] = fmaf(acc[0], sc[0][G], s[i][nt][0]);
-                        s[i][nt][1] = fmaf(acc[1], sc[0][G], s[i][nt][1]);
-                        s[i][nt][2] = fmaf(acc[2], sc[1][G], s[i][nt][2]);
-                        s[i][nt][3] = fmaf(acc[3], sc[1][G], s[i][nt][3]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[i][nt][e] = G ? fmaf(acc[e], sc[e >> 1][G], s[i][nt][e]) : acc[e] * sc[e >> 1][G];
                     }
                 }
             }
@@ -537,9 +601,10 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                        float acc[4];
+                        mma16816_first(acc, A[0][0][0], A[1][0][0], A[0][1][0], A[1][1][0], pf[nt][0], pf[nt][4]);
 #pragma unroll
-                        for (int x = 0; x < 4; ++x)
+                        for (int x = 1; x < 4; ++x)
                             mma16816(acc, A[0][0][x], A[1][0][x], A[0][1][x], A[1][1][x], pf[nt][x], pf[nt][4 + x]);
                         o[j][nt][0] = fmaf(acc[0], sc[0], o[j][nt][0]);
                         o[j][nt][1] = fmaf(acc[1], sc[0], o[j][nt][1]);
@@ -564,6 +629,8 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
                 for (int x = 4; x < 32; x <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], x);
         remaining -= n_here;
         const bool begins = first_p == 0, ends = first_p + n_here == cur.np;
+        if (begins && a.seg_ctas && lane == 0)                      // for the page weights: the CTAs that hold the segment
+            a.seg_ctas[(long long)cur.b * U + cur.u] = make_int2(blockIdx.x, Shares(total, ctas).owner(seg_at + 2 * cur.np - 1));
         if (begins && ends) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -606,13 +673,14 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
             }
         }
         // next segment
-        seg_at += cur.np;
+        seg_at += steps_of(cur.np);
         cur.p = 0;
         if (ends && remaining > 0) {
             if (++cur.u == U) {
                 cur.u = 0;
                 do { ++cur.b; } while (cur.b < c.B && (cur.np = c.n_pages_of(cur.b)) == 0);
             }
+            ql.template issue<ROWS>(a, cur, g, t);
         }
     }
     if (!ok) {
@@ -620,112 +688,132 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
         if (lane == 0 && c.d_status) *c.d_status = HIFA4_ERR_TIMEOUT;
         let_copies_land();
     }
-    // ---- pieces that warps share: a (segment, row) per warp and turn
+    // ---- pieces that warps share: a row of a segment per warp and turn
     __syncthreads();
-    {
-        const long long at = lane < 2 * W ? piece_at[lane] : -1;
-        const unsigned first = __ballot_sync(0xffffffffu, !(lane & 1) && at >= 0 && at < cta0);   // of the segment that the CTA before began
-        unsigned leaders = __ballot_sync(0xffffffffu, (lane & 1) && at >= 0) | (first & (0u - first));
-        int unit = 0;
-        while (leaders) {
-            const int lead = __ffs(leaders) - 1;
-            leaders &= leaders - 1;
-            const long long seg = __shfl_sync(0xffffffffu, at, lead);
-            const unsigned members = __ballot_sync(0xffffffffu, !(lane & 1) && at == seg) | (1u << lead);
-            const Cursor sg = piece[lead];
-            const bool whole = seg >= cta0 && seg + sg.np <= cta1;
-            const int ws = 2 * (int)blockIdx.x + (seg < cta0 ? 0 : 1);
-            const bool mine = members >> lane & 1;
-            const float* const po = mine ? piece_of[lane] : nullptr;
+    const int at = lane < 2 * W ? piece_at[lane] : -1;
+    const bool second = lane & 1;
+    const unsigned first = __ballot_sync(0xffffffffu, !second && at >= 0 && at + 1 < cta0);      // of the segment that a CTA before began
+    unsigned leaders = __ballot_sync(0xffffffffu, second && at >= 0) | (first & (0u - first));
+    const unsigned cross = __ballot_sync(0xffffffffu, second && at >= 0 && at + 2 * piece[lane].np - 1 >= cta1);
+    if (tid == 0) {                                                  // what the join finds here
+        int4 x = make_int4(-1, 0, 0, 0);
+        if (cross) {
+            const Cursor sg = piece[__ffs(cross) - 1];
+            x = make_int4(sg.b, sg.u, Shares(total, ctas).owner(piece_at[__ffs(cross) - 1] + 2 * sg.np - 1), 0);
+        }
+        a.begun[blockIdx.x] = x;
+    }
+    int turn = warp;
+    while (leaders) {
+        const int lead = __ffs(leaders) - 1;
+        leaders &= leaders - 1;
+        const int seg = __shfl_sync(0xffffffffu, at, lead);
+        const unsigned members = __ballot_sync(0xffffffffu, !second && at == seg) | (1u << lead);
+        const Cursor sg = piece[lead];
+        const bool begun_here = seg + 1 >= cta0, whole = begun_here && seg + 2 * sg.np - 1 < cta1, mine = members >> lane & 1;
+        const int ws = 2 * (int)blockIdx.x + (begun_here ? 1 : 0);
+        const int kv = kv_of(a, sg.u), rows = min(ROWS, (a.units.first[kv + 1] - a.units.first[kv]) * a.N - (sg.u - kv * a.blocks) * ROWS);
 #pragma unroll 1
-            for (int r = 0; r < ROWS; ++r) {
+        for (; turn < rows; turn += W + 1) {
+            const int r = turn;
+            const float* const po = piece_of[mine ? lane : lead];
+            const float m = mine ? po[ROWS * D + 2 * r] : -INFINITY, l = mine ? po[ROWS * D + 2 * r + 1] : 0.f;
+            const float M = warp_max(m), f = rebase(m, M), L = warp_sum(l * f);
+            float o[D / 32];
+#pragma unroll
+            for (int y = 0; y < D / 32; ++y) o[y] = 0.f;
+            for (unsigned rest = members; rest;) {                   // two pieces at a time
+                const int x0 = __ffs(rest) - 1;
+                rest &= rest - 1;
+                const int x1 = rest ? __ffs(rest) - 1 : x0;
+                const float f0 = __shfl_sync(0xffffffffu, f, x0), f1 = rest ? __shfl_sync(0xffffffffu, f, x1) : 0.f;
+                rest &= rest - 1;
+                const float *p0 = piece_of[x0] + r * D + lane, *p1 = piece_of[x1] + r * D + lane;
+                float v0[D / 32], v1[D / 32];
+#pragma unroll
+                for (int y = 0; y < D / 32; ++y) { v0[y] = p0[32 * y]; v1[y] = p1[32 * y]; }
+#pragma unroll
+                for (int y = 0; y < D / 32; ++y) o[y] = fmaf(v1[y], f1, fmaf(v0[y], f0, o[y]));
+            }
+            if (whole) {
                 int head, tok;
-                if (!row_of<ROWS>(a, sg.u, r, head, tok)) break;
-                if (unit++ % (W + 1) != warp) continue;
-                const float m = mine ? po[ROWS * D + 2 * r] : -INFINITY;
-                const float M = warp_max(m), f = rebase(m, M);
-                const float L = warp_sum(mine ? po[ROWS * D + 2 * r + 1] * f : 0.f);
-                float o[D / 32];
+                row_of<ROWS>(a, sg.u, r, head, tok);
+                const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
-                for (int x = 0; x < D / 32; ++x) o[x] = 0.f;
-                for (unsigned rest = members; rest; rest &= rest - 1) {
-                    const int x = __ffs(rest) - 1;
-                    const float fx = __shfl_sync(0xffffffffu, f, x);
-                    const float* px = piece_of[x] + r * D + lane;
+                for (int y = 0; y < D / 32; ++y) store_out(a, sg.b, head, tok, D, 32 * y + lane, o[y] * inv);
+                if (lane == 0) store_row_stats(a, sg.b, head, tok, M, L);
+            } else {
+                float* dst = a.part_o + ((long long)ws * ROWS + r) * D + lane;
 #pragma unroll
-                    for (int y = 0; y < D / 32; ++y) o[y] = fmaf(px[32 * y], fx, o[y]);
-                }
-                if (whole) {
-                    const float inv = L == 0.f ? 0.f : 1.f / L;
-#pragma unroll
-                    for (int y = 0; y < D / 32; ++y) store_out(a, sg.b, head, tok, D, 32 * y + lane, o[y] * inv);
-                    if (lane == 0) store_row_stats(a, sg.b, head, tok, M, L);
-                } else {
-                    float* dst = a.part_o + ((long long)ws * ROWS + r) * D + lane;
-#pragma unroll
-                    for (int y = 0; y < D / 32; ++y) dst[32 * y] = o[y];
-                    if (lane == 0) a.part_ml[(long long)ws * ROWS + r] = make_float2(M, L);
-                }
+                for (int y = 0; y < D / 32; ++y) dst[32 * y] = o[y];
+                if (lane == 0) a.part_ml[(long long)ws * ROWS + r] = make_float2(M, L);
             }
         }
+        turn -= rows;
     }
 }
 
-// CTAs [0, DECODE_CTAS): the segment that begins in the CTA of this number and goes on in others, joined from their partial sums (a
-// group of JOIN_WARPS / 8 warps per row, eight rows at a time), and the sequences without keys.  The rest: page weights, 64
-// pages of a sequence each: sum over the query heads of (sum of p in the page) / (sum of p in all pages).
+// The first JOIN_PARTS * DECODE_CTAS CTAs: the segment that begins in CTA c0 of the decode kernel and goes on in others, joined from
+// their partial sums (32 channels of a row per warp), and the sequences without keys.  The rest: page weights, 64 pages of
+// a sequence each: sum over the query heads of (sum of p in the page) / (sum of p in all pages).
 constexpr int JOIN_WARPS = 16;
+template <int D, int ROWS> constexpr int JOIN_PARTS = ROWS * D / 32 / JOIN_WARPS;
 template <int D, int ROWS>
 __global__ void __launch_bounds__(JOIN_WARPS * 32)
 cache_join_kernel(const __grid_constant__ DecodeArgs a)
 {
-    constexpr int GROUP = JOIN_WARPS / 8;
-    __shared__ long long scratch[JOIN_WARPS];
-    __shared__ float part[JOIN_WARPS][D];
+    __shared__ float sums[JOIN_WARPS * 32];
     __shared__ float2 ml_of[HIFA4_MAX_HEADS];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const CacheView& c = a.cache;
     const int U = units_per_seq(a), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const long long total = pages_before(c, c.B, scratch) * U;
-    const int ctas = active_ctas(total);
-    if (blockIdx.x >= DECODE_CTAS) {
-        const int chunks = (c.max_pages + 63) / 64, w = (int)blockIdx.x - DECODE_CTAS, b = w / chunks, p0 = w % chunks * 64;
+    // the piece of a segment in CTA x: slot 1 where it begins (x = c0), else slot 0
+    auto slot_of = [](int x, int c0) { return (2ll * x + (x == c0 ? 1 : 0)) * ROWS; };
+    if (blockIdx.x >= JOIN_PARTS<D, ROWS> * DECODE_CTAS) {
+        const int chunks = (c.max_pages + 63) / 64, w = (int)blockIdx.x - JOIN_PARTS<D, ROWS> * DECODE_CTAS, b = w / chunks, p0 = w % chunks * 64;
         const int np = c.n_pages_of(b);
         if (p0 >= np) return;
-        const long long before = pages_before(c, b, scratch) * U;
+        const int p = p0 + (tid & 63), grp = tid >> 6;
+        constexpr int GROUPS = JOIN_WARPS / 2, AHEAD = 4;
+        const float2* src = a.page_ml + (long long)b * a.Hq * c.max_pages + p;
+        float2 pre[AHEAD];                                           // of the first heads, asked for ahead of the sums
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            pre[i] = p < np && grp + i * GROUPS < a.Hq ? src[(long long)(grp + i * GROUPS) * c.max_pages] : make_float2(-INFINITY, 0.f);
         for (int j = tid; j < a.Hq; j += JOIN_WARPS * 32) {          // j: place among the query heads sorted by KV head
             int kv = 0;
             while (a.units.first[kv + 1] <= j) ++kv;
             const int in = j - a.units.first[kv], head = a.units.head[j], r = in % ROWS;
-            const long long at = before + (long long)(kv * a.blocks + in / ROWS) * np;
-            const long long c0 = ((at + 1) * ctas - 1) / total, c1 = ((at + np) * ctas - 1) / total;
+            const int2 cc = a.seg_ctas[(long long)b * U + kv * a.blocks + in / ROWS];
             float2 ml;
-            if (c0 == c1) {
+            if (cc.x == cc.y) {
                 ml = a.final_ml[(long long)b * a.Hq + head];
             } else {
                 ml = make_float2(-INFINITY, 0.f);
-                for (long long x = c0; x <= c1; ++x) ml.x = fmaxf(ml.x, a.part_ml[(2 * x + (x == c0)) * ROWS + r].x);
-                for (long long x = c0; x <= c1; ++x) {
-                    const float2 y = a.part_ml[(2 * x + (x == c0)) * ROWS + r];
+                for (int x = cc.x; x <= cc.y; ++x) ml.x = fmaxf(ml.x, a.part_ml[slot_of(x, cc.x) + r].x);
+                for (int x = cc.x; x <= cc.y; ++x) {
+                    const float2 y = a.part_ml[slot_of(x, cc.x) + r];
                     ml.y = fmaf(y.y, rebase(y.x, ml.x), ml.y);
                 }
             }
             ml_of[head] = make_float2(ml.x, ml.y == 0.f ? 0.f : 1.f / ml.y);
         }
         __syncthreads();
-        const int p = p0 + (tid & 63), grp = tid >> 6;
-        constexpr int GROUPS = JOIN_WARPS / 2;
         float w_sum = 0.f;
         if (p < np) {
-            const float2* src = a.page_ml + (long long)b * a.Hq * c.max_pages + p;
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (grp + i * GROUPS < a.Hq) {
+                    const float2 all = ml_of[grp + i * GROUPS];
+                    w_sum = fmaf(pre[i].y * rebase(pre[i].x, all.x), all.y, w_sum);
+                }
 #pragma unroll 4
-            for (int h = grp; h < a.Hq; h += GROUPS) {
+            for (int h = grp + AHEAD * GROUPS; h < a.Hq; h += GROUPS) {
                 const float2 ml = src[(long long)h * c.max_pages], all = ml_of[h];
                 w_sum = fmaf(ml.y * rebase(ml.x, all.x), all.y, w_sum);
             }
         }
-        float* sums = &part[0][0];
         sums[tid] = w_sum;
         __syncthreads();
         if (grp == 0 && p < np) {
@@ -736,6 +824,45 @@ cache_join_kernel(const __grid_constant__ DecodeArgs a)
         }
         return;
     }
+    constexpr int CHUNKS = (DECODE_CTAS + 31) / 32, AHEAD = 8;
+    const int c0 = blockIdx.x % DECODE_CTAS, turn = blockIdx.x / DECODE_CTAS * JOIN_WARPS + warp, r = turn / (D / 32), ch = turn % (D / 32) * 32 + lane;
+    const int4 sg = a.begun[c0];
+    // asked for before it is known whether there is a segment and how long it is
+    float2 ml[CHUNKS];
+    ml[0] = a.part_ml[slot_of(min(c0 + lane, DECODE_CTAS - 1), c0) + r];
+    float o_first[AHEAD];
+#pragma unroll
+    for (int x = 0; x < AHEAD; ++x) o_first[x] = a.part_o[(slot_of(min(c0 + x, DECODE_CTAS - 1), c0) + r) * D + ch];
+    int head, tok;
+    if (sg.x >= 0 && row_of<ROWS>(a, sg.y, r, head, tok)) {
+        const int n = sg.z - c0 + 1;
+        float M = -INFINITY, L = 0.f, o = 0.f;
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+            if (32 * i + lane >= n) ml[i] = make_float2(-INFINITY, 0.f);
+            else if (i) ml[i] = a.part_ml[slot_of(c0 + 32 * i + lane, c0) + r];
+            M = fmaxf(M, ml[i].x);
+        }
+        M = warp_max(M);
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+            const float f = rebase(ml[i].x, M);
+            L = fmaf(ml[i].y, f, L);
+            const int most = min(32, n - 32 * i);
+            const float* src = a.part_o + (2ll * (c0 + 32 * i) * ROWS + r) * D + ch;
+            int x = 0;
+            if (i == 0) {
+#pragma unroll
+                for (; x < AHEAD; ++x) o = fmaf(x < n ? o_first[x] : 0.f, __shfl_sync(0xffffffffu, f, x), o);
+            }
+#pragma unroll 8
+            for (; x < most; ++x) o = fmaf(src[2ll * x * ROWS * D], __shfl_sync(0xffffffffu, f, x), o);
+        }
+        L = warp_sum(L);
+        store_out(a, sg.x, head, tok, D, ch, L == 0.f ? 0.f : o / L);
+        if (ch == 0) store_row_stats(a, sg.x, head, tok, M, L);
+    }
+    if (blockIdx.x >= DECODE_CTAS) return;
     for (int b = blockIdx.x; b < c.B; b += DECODE_CTAS) {            // no keys: zeros
         if (c.n_pages_of(b) > 0) continue;
         if (tid == 0 && c.len(b) < 0) c.invalid();
@@ -743,53 +870,6 @@ cache_join_kernel(const __grid_constant__ DecodeArgs a)
             const int head = i / (a.N * D), tok = i / D % a.N;
             store_out(a, b, head, tok, D, i % D, 0.f);
             if (i % D == 0) store_row_stats(a, b, head, tok, -INFINITY, 0.f);
-        }
-    }
-    if ((int)blockIdx.x + 1 >= ctas) return;                          // nothing goes on behind the last CTA
-    const long long cta0 = total * blockIdx.x / ctas, cta1 = total * (blockIdx.x + 1) / ctas;
-    const Cursor sg = locate(c, U, cta1 - 1, lane);
-    const long long at = cta1 - 1 - sg.p;
-    if (at < cta0 || at + sg.np == cta1) return;
-    const int c0 = blockIdx.x, n = (int)(((at + sg.np) * ctas - 1) / total) - c0 + 1;
-    const int per = (n + GROUP - 1) / GROUP, x0 = min(n, warp % GROUP * per), x1 = min(n, x0 + per);
-    auto slot_of = [&](int x) { return (long long)(2 * (c0 + x) + (x == 0 ? 1 : 0)) * ROWS; };
-#pragma unroll 1
-    for (int r0 = 0; r0 < ROWS; r0 += 8) {
-        const int r = r0 + warp / GROUP;
-        int head, tok;
-        const bool have = row_of<ROWS>(a, sg.u, r, head, tok);
-        float M = -INFINITY, L = 0.f, o[D / 32];
-#pragma unroll
-        for (int y = 0; y < D / 32; ++y) o[y] = 0.f;
-        if (have) {
-            for (int x = lane; x < n; x += 32) M = fmaxf(M, a.part_ml[slot_of(x) + r].x);
-            M = warp_max(M);
-            for (int x = lane; x < n; x += 32) {
-                const float2 ml = a.part_ml[slot_of(x) + r];
-                L = fmaf(ml.y, rebase(ml.x, M), L);
-            }
-            L = warp_sum(L);
-#pragma unroll 8
-            for (int x = x0; x < x1; ++x) {
-                const float f = rebase(a.part_ml[slot_of(x) + r].x, M);
-                const float* src = a.part_o + (slot_of(x) + r) * D + lane;
-#pragma unroll
-                for (int y = 0; y < D / 32; ++y) o[y] = fmaf(src[32 * y], f, o[y]);
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int y = 0; y < D / 32; ++y) part[warp][32 * y + lane] = o[y];
-        __syncthreads();
-        if (have && warp % GROUP == 0) {
-            const float inv = L == 0.f ? 0.f : 1.f / L;
-#pragma unroll
-            for (int y = 0; y < D / 32; ++y) {
-#pragma unroll
-                for (int x = 1; x < GROUP; ++x) o[y] += part[warp + x][32 * y + lane];
-                store_out(a, sg.b, head, tok, D, 32 * y + lane, o[y] * inv);
-            }
-            if (lane == 0) store_row_stats(a, sg.b, head, tok, M, L);
         }
     }
 }
@@ -807,7 +887,7 @@ static cudaError_t decode_nt(const DecodeArgs& a, cudaStream_t st)
     const cudaError_t e = launch_dependent(cache_decode_kernel<T, D, NT>, DECODE_CTAS, C::THREADS, C::SMEM, st, a);
     if (e != cudaSuccess) return e;
     const unsigned weight_blocks = a.weight_out ? (unsigned)a.cache.B * ((unsigned)(a.cache.max_pages + 63) / 64) : 0;
-    return launch_dependent(cache_join_kernel<D, C::ROWS>, DECODE_CTAS + weight_blocks, JOIN_WARPS * 32, 0, st, a);
+    return launch_dependent(cache_join_kernel<D, C::ROWS>, JOIN_PARTS<D, C::ROWS> * DECODE_CTAS + weight_blocks, JOIN_WARPS * 32, 0, st, a);
 }
 
 template <typename T>
