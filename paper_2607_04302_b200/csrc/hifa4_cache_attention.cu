@@ -14,7 +14,9 @@
 // The reference of a row moves only when its maximum exceeds it by more than 2^8: P stays below 2^8, FP32 sums hold, and O is
 // rarely rescaled.
 //
-// Warps: 0-3 (and 4-7) softmax of a tile, one thread per row; the next four dequantize; then the issuer of the MMAs and the loader.
+// Warps: 0-3 (and 4-7) softmax of a tile, one thread per row; the next four dequantize; then an issuer of MMAs per tile, which waits
+// for its tile alone and suspended in hardware (one that polls for both tiles takes issue slots from the softmax warps of its
+// scheduler, one that takes them in turn makes each wait for the other), and the loader.
 // S is released as soon as it is in registers, so that the next S is formed under the softmax; P has columns of its own.  Order
 // among MMAs of different shapes is not relied on: every reuse of tensor memory waits for a commit.
 #include "hifa4_cache.cuh"
@@ -30,7 +32,7 @@ template <int D, bool SPLIT> struct TileCfg {
     static constexpr int S_COL = QT * D, P_COL = S_COL + QT * 64, Q_COL = P_COL + QT * P_COLS;
     static constexpr int Q_FIT = (512 - Q_COL) / (D / 2);
     static constexpr int Q_SMEM = QT * TERMS > Q_FIT ? QT * TERMS - Q_FIT : 0;      // (tile, term) pairs, the last ones
-    static constexpr int SMW = 4 * QT, W_DQ = SMW, W_MMA = SMW + 4, W_LD = SMW + 5, THREADS = (SMW + 6) * 32;
+    static constexpr int SMW = 4 * QT, W_DQ = SMW, W_MMA = SMW + 4, W_LD = W_MMA + QT, THREADS = (W_LD + 1) * 32;
     static constexpr int KS = D == 256 ? 2 : 3;                          // stages of K and V tiles
     static constexpr int RS = D == 256 ? (SPLIT ? 1 : 2) : 3;            // of raw pages
     static constexpr int K_STAGE = 64 * D * 2, V_STAGE = D * 128, Q_TERM = 128 * D * 2;
@@ -106,8 +108,8 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
     if (tid == 0) {
         for (int i = 0; i < 3; ++i) {
             mbar_init(bar(RF + i), 1); mbar_init(bar(RE + i), 4);
-            mbar_init(bar(KF + i), 4); mbar_init(bar(KE + i), 1);
-            mbar_init(bar(VF + i), 4); mbar_init(bar(VE + i), 1);
+            mbar_init(bar(KF + i), 4); mbar_init(bar(KE + i), C::QT);
+            mbar_init(bar(VF + i), 4); mbar_init(bar(VE + i), C::QT);
         }
         mbar_init(bar(QF), C::SMW);
         for (int i = 0; i < 2; ++i) { mbar_init(bar(SF + i), 1); mbar_init(bar(SR + i), 4); mbar_init(bar(PF + i), 4); mbar_init(bar(OD + i), 1); }
@@ -380,64 +382,63 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
             __syncwarp();
             if (lane == 0) { mbar_arrive(bar(VF + ks)); mbar_arrive(bar(RE + rs)); }
         }
-    } else if (warp == C::W_MMA) {
-        // ------------------------------------------------------------------ MMAs
+    } else if (warp < C::W_LD) {
+        // ------------------------------------------------------------------ MMAs of a tile
+        const int h = warp - C::W_MMA;
         if (n > 0 && elect_one()) {
             constexpr uint32_t ID_S = umma_idesc_bf16(128, 64), ID_O = umma_idesc_bf16(128, D);
             bool good = tile_wait(bar(QF), 0, &abort_flag);
             tc_fence_after();
-            auto scores = [&](int h, int j) {                        // S(j) of tile h
-                const uint32_t kl = umma_desc_lo(smem + (j % C::KS) * C::K_STAGE);
+#pragma unroll 1
+            for (int j = 0; j <= n && good; ++j) {
+                if (j < n) {                                         // S(j)
+                    good = tile_wait(bar(KF + j % C::KS), (uint32_t)(j / C::KS) & 1u, &abort_flag) &&
+                           (j == 0 || h >= tiles || tile_wait(bar(SR + h), (uint32_t)(j - 1) & 1u, &abort_flag));
+                    if (!good) break;
+                    tc_fence_after();
+                    if (h < tiles) {
+                        const uint32_t kl = umma_desc_lo(smem + (j % C::KS) * C::K_STAGE), d = tmem + C::S_COL + 64 * h;
 #pragma unroll
-                for (int term = 0; term < C::TERMS; ++term) {
-                    const int i = h * C::TERMS + term;
-                    const uint32_t ql = umma_desc_lo(smem + C::Q_OFF + (i - C::Q_FIT) * C::Q_TERM);
+                        for (int term = 0; term < C::TERMS; ++term) {
+                            const int i = h * C::TERMS + term;
+                            const uint32_t qt = tmem + C::Q_COL + i * (D / 2), ql = umma_desc_lo(smem + C::Q_OFF + (i - C::Q_FIT) * C::Q_TERM);
+                            if (i < C::Q_FIT) {
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t d = tmem + C::S_COL + 64 * h, bd = kl + (k / 4) * (8192 >> 4) + (k % 4) * 2;
-                        if (i < C::Q_FIT) umma_bf16_ts_lo(d, tmem + C::Q_COL + i * (D / 2) + 8 * k, bd, ID_S, term + k > 0);
-                        else umma_bf16_ss_lo(d, ql + (k / 4) * (16384 >> 4) + (k % 4) * 2, bd, ID_S, term + k > 0);
+                                for (int k = 0; k < D / 16; ++k)
+                                    umma_bf16_ts_lo(d, qt + 8 * k, kl + (k / 4) * (8192 >> 4) + (k % 4) * 2, ID_S, term + k > 0);
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < D / 16; ++k)
+                                    umma_bf16_ss_lo(d, ql + (k / 4) * (16384 >> 4) + (k % 4) * 2, kl + (k / 4) * (8192 >> 4) + (k % 4) * 2, ID_S,
+                                                    term + k > 0);
+                            }
+                        }
+                        umma_commit(bar(SF + h));
+                        umma_commit(bar(KE + j % C::KS));
+                    } else {
+                        mbar_arrive(bar(KE + j % C::KS));            // a tile without rows holds nothing up
                     }
                 }
-                umma_commit(bar(SF + h));
-            };
-            auto output = [&](int h, int j) {                        // O += P(j) V(j) of tile h
-                const uint32_t vl = umma_desc_lo(smem + C::V_OFF + (j % C::KS) * C::V_STAGE);
+                if (j > 0) {                                         // O += P(j - 1) V(j - 1)
+                    const int i = j - 1;
+                    good = tile_wait(bar(VF + i % C::KS), (uint32_t)(i / C::KS) & 1u, &abort_flag) &&
+                           (h >= tiles || tile_wait(bar(PF + h), (uint32_t)i & 1u, &abort_flag));
+                    if (!good) break;
+                    tc_fence_after();
+                    if (h < tiles) {
+                        const uint32_t vl = umma_desc_lo(smem + C::V_OFF + (i % C::KS) * C::V_STAGE);
 #pragma unroll
-                for (int term = 0; term < C::TERMS; ++term)
+                        for (int term = 0; term < C::TERMS; ++term)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        umma_bf16_ts_lo(tmem + h * D, tmem + C::P_COL + C::P_COLS * h + term * 32 + 8 * k, vl + 2 * k, ID_O, j > 0 || term + k > 0);
-                umma_commit(bar(OD + h));
-            };
-            // whichever product is ready, tiles in turn; a K (V) tile is released behind the last tile's product with it
-            int nq[2] = {0, tiles > 1 ? 0 : n}, nv[2] = {0, tiles > 1 ? 0 : n}, ke = 0, ve = 0;
-            uint32_t idle = 0;
-            while (good && (nv[0] < n || nv[1] < n)) {
-                bool any = false;
-#pragma unroll
-                for (int h = 0; h < C::QT; ++h) {
-                    const int j = nq[h];
-                    if (j < n && mbar_test_wait(bar(KF + j % C::KS), (uint32_t)(j / C::KS) & 1u) &&
-                        (j == 0 || mbar_test_wait(bar(SR + h), (uint32_t)(j - 1) & 1u))) {
-                        tc_fence_after();
-                        scores(h, j);
-                        ++nq[h];
-                        any = true;
-                        if (min(nq[0], nq[1]) > ke) { umma_commit(bar(KE + ke % C::KS)); ++ke; }
-                    }
-                    const int i = nv[h];
-                    if (i < nq[h] && i < n && mbar_test_wait(bar(PF + h), (uint32_t)i & 1u) &&
-                        mbar_test_wait(bar(VF + i % C::KS), (uint32_t)(i / C::KS) & 1u)) {
-                        tc_fence_after();
-                        output(h, i);
-                        ++nv[h];
-                        any = true;
-                        if (min(nv[0], nv[1]) > ve) { umma_commit(bar(VE + ve % C::KS)); ++ve; }
+                            for (int k = 0; k < 4; ++k)
+                                umma_bf16_ts_lo(tmem + h * D, tmem + C::P_COL + C::P_COLS * h + term * 32 + 8 * k, vl + 2 * k, ID_O,
+                                                i > 0 || term + k > 0);
+                        umma_commit(bar(OD + h));
+                        umma_commit(bar(VE + i % C::KS));
+                    } else {
+                        mbar_arrive(bar(VE + i % C::KS));
                     }
                 }
-                idle = any ? 0 : idle + 1;
-                if ((idle & 63u) == 63u && (abort_flag || idle > 64 * POLLS)) good = false;
             }
             // the last commits have arrived before this shared memory goes to another CTA
             if (good) good = tile_wait(bar(KE + (n - 1) % C::KS), (uint32_t)((n - 1) / C::KS) & 1u, &abort_flag) &&
