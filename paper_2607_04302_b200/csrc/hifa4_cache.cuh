@@ -100,10 +100,10 @@ struct TileArgs {
     const float* s;
     int Hq, N, causal, out_dtype;
     int items;                         // row blocks per KV head
-    int splits;
+    int full, splits;                  // blocks [0, full) have a CTA each, the others `splits` CTAs
     float scale_log2;
     void* out;
-    float* part_o;                     // [(sequence, KV head, item, tile), split][128][d] (splits > 1)
+    float* part_o;                     // [block - full][tile][split][128][d]
     float2* part_ml;
 };
 

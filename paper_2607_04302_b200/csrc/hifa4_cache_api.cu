@@ -166,22 +166,38 @@ int run_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cac
                                                                                                                   : HIFA4_ERR_CUDA;
 }
 
-// The tensor-memory kernel's grid and workspace.
+// The tensor-memory kernel's grid and workspace.  A CTA has an SM to itself; blocks come in waves, and a last wave that does not
+// fill the chip takes as long as a full one: the blocks behind the last full wave (or the one before) are split over their pages
+// where that shortens the whole.  In units of a page (1 us): a CTA's prologue and epilogue cost 6, joining 6 (four sequences of 5-8K
+// tokens, 512 blocks: split in two behind three waves 434 us, in thirteen 507, not split 450; 96 blocks of 1500 tokens
+// at most: not split 23, in three 32).
 struct TileLayout {
-    long long items, blocks;
+    long long items, blocks, full;
     int splits;
     size_t part_ml, total;
     TileLayout(const hifa4_cache* c, int B, int max_pages, int rows)
     {
-        const int block = attention_tile_rows(c->in_dtype, c->d);
+        const int block = attention_tile_rows(c->in_dtype, c->d), sms = DECODE_CTAS;
         items = (rows + block - 1) / block;
         blocks = (long long)B * c->Hkv * items;
+        full = blocks;
         splits = 1;
-        if (blocks < DECODE_CTAS) splits = (int)(DECODE_CTAS / blocks);
-        const int most = max_pages / 8 > 1 ? max_pages / 8 : 1;
-        if (splits > most) splits = most;
-        part_ml = splits > 1 ? align256((size_t)blocks * block * splits * c->d * sizeof(float)) : 0;
-        total = splits > 1 ? part_ml + align256((size_t)blocks * block * splits * sizeof(float2)) : 0;
+        const double fixed = 6.0, pages = max_pages;
+        double best = (double)((blocks + sms - 1) / sms) * (pages + fixed);
+        for (long long waves = blocks / sms; waves >= 0 && waves >= blocks / sms - 1; --waves) {
+            const long long rest = blocks - waves * sms;
+            for (int s = 2; rest > 0 && s <= 32; ++s) {
+                const double t = waves * (pages + fixed) + (double)((rest * s + sms - 1) / sms) * (pages / s + fixed) + fixed;
+                if (t < best) {
+                    best = t;
+                    full = waves * sms;
+                    splits = s;
+                }
+            }
+        }
+        const size_t pieces = (size_t)(blocks - full) * splits;
+        part_ml = align256(pieces * block * c->d * sizeof(float));
+        total = part_ml + align256(pieces * block * sizeof(float2));
     }
 };
 
@@ -278,7 +294,7 @@ int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, cons
         return run_decode(cache, seqs, query, units, rows, qs, q, s, out, nullptr, nullptr, nullptr, workspace, workspace_bytes, d_status, stream);
     const TileLayout lay(cache, seqs->B, seqs->max_pages, rows);
     if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;
-    if (lay.blocks * lay.splits * 32 > 0x7FFFFFFFll) return HIFA4_ERR_UNSUPPORTED;
+    if (lay.blocks * 32 * lay.splits > 0x7FFFFFFFll) return HIFA4_ERR_UNSUPPORTED;
     if ((rc = check_arch())) return rc;
     TileArgs a;
     std::memset(&a, 0, sizeof(a));
@@ -286,6 +302,7 @@ int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, cons
     a.units = units;
     a.qs = qs;
     a.items = (int)lay.items;
+    a.full = (int)lay.full;
     a.splits = lay.splits;
     a.part_o = (float*)workspace;
     a.part_ml = (float2*)((char*)workspace + lay.part_ml);

@@ -2,9 +2,11 @@
 //
 //   S = Q~ K^T scale,  m = running reference,  P = exp2(S log2e - m),  O += P V,  l += sum P,  out = O / l
 //
-// One CTA per 256 (QT = 2) or 128 query rows of one KV head and sequence, or per a share of the sequence's pages when there are too
-// few of them to fill the chip (joined by a second kernel).  Rows are (query head, token) pairs in the order of the heads, so
-// that short queries of several heads fill a tile.  Key tiles are pages.
+// One CTA per 256 (QT = 2) or 128 query rows of one KV head and sequence, or per a share of the sequence's pages for the blocks of
+// a last wave that would not fill the chip (joined by a second kernel).  Rows are (query head, token) pairs in the order of the
+// heads, so that short queries of several heads fill a tile.  Key tiles are pages.  With 128 rows or fewer to a CTA of two tiles,
+// both take the same rows, one the even and one the odd pages, and are joined in shared memory: what bounds such a CTA is the
+// chain of a tile from page to page.
 //
 // Both products take the exact BF16 values of the cache, which dequantization warps write to shared memory from the pages' codes:
 // an image of the cache in global memory would be 3.5 times its size, and only 15 instructions per 8 values are needed, a quarter
@@ -19,6 +21,8 @@
 // scheduler, one that takes them in turn makes each wait for the other), and the loader.
 // S is released as soon as it is in registers, so that the next S is formed under the softmax; P has columns of its own.  Order
 // among MMAs of different shapes is not relied on: every reuse of tensor memory waits for a commit.
+#include <type_traits>
+
 #include "hifa4_cache.cuh"
 #include "hifa4_ptx.cuh"
 
@@ -47,6 +51,7 @@ namespace tilek {
 // registers, PF P stored, OD O complete.
 enum { RF = 0, RE = 3, KF = 6, KE = 9, VF = 12, VE = 15, QF = 18, SF = 20, SR = 22, PF = 24, OD = 26, N_BARS = 28 };
 constexpr uint32_t POLLS = 1u << 18;
+constexpr int POLY = 1;
 }  // namespace tilek
 
 __device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity, volatile int* abort)
@@ -57,6 +62,29 @@ __device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity, volatil
         if ((i & 63u) == 63u && *abort) return false;
     }
     return false;
+}
+
+// Two exponentials to base 2 on the multiply-add pipe, for -126 <= x (less counts as -126) and x < 127: x = n + f with n the nearest
+// integer (by adding 1.5 * 2^23, whose low bits then hold n), 2^f by the polynomial of degree 5 that has the least largest relative
+// error on [-1/2, 1/2] (fitted by reweighted least squares; 2.1e-7 with FP32 coefficients and Horner steps), n added to the exponent.
+__device__ __forceinline__ void exp2_pair(float& x0, float& x1)
+{
+    const uint64_t magic = pack2(12582912.f, 12582912.f), unmagic = pack2(-12582912.f, -12582912.f), minus = pack2(-1.f, -1.f);
+    const uint64_t x = pack2(fmaxf(x0, -126.f), fmaxf(x1, -126.f)), t = add2(x, magic), f = fma2(add2(t, unmagic), minus, x);
+    uint64_t p = pack2(0.0013276472454890609f, 0.0013276472454890609f);
+    p = fma2(p, f, pack2(0.009675540961325169f, 0.009675540961325169f));
+    p = fma2(p, f, pack2(0.05550713092088699f, 0.05550713092088699f));
+    p = fma2(p, f, pack2(0.24022120237350464f, 0.24022120237350464f));
+    p = fma2(p, f, pack2(0.6931469440460205f, 0.6931469440460205f));
+    p = fma2(p, f, pack2(1.0000001192092896f, 1.0000001192092896f));
+    float p0, p1, t0, t1;
+    unpack2(p, p0, p1);
+    unpack2(t, t0, t1);
+    uint32_t r0, r1;
+    asm("mad.lo.u32 %0, %1, 0x800000, %2;" : "=r"(r0) : "r"(__float_as_uint(t0)), "r"(__float_as_uint(p0)));
+    asm("mad.lo.u32 %0, %1, 0x800000, %2;" : "=r"(r1) : "r"(__float_as_uint(t1)), "r"(__float_as_uint(p1)));
+    x0 = __uint_as_float(r0);
+    x1 = __uint_as_float(r1);
 }
 
 __device__ __forceinline__ void tile_store(const TileArgs& a, long long i, float x, float y)
@@ -124,8 +152,13 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
     const uint32_t tmem = tmem_slot;
 
     const CacheView& c = a.cache;
-    int w = blockIdx.x;
-    const int sp = w % a.splits; w /= a.splits;
+    int w = blockIdx.x, sp = 0, splits = 1;
+    if (w >= a.full) {                                               // a block of the last wave: its pages are shared out
+        splits = a.splits;
+        sp = (w - a.full) % splits;
+        w = a.full + (w - a.full) / splits;
+    }
+    const int slot = w - a.full;                                     // of its partial results
     const int item = a.items - 1 - w % a.items; w /= a.items;        // causal: the longest rows first
     const int kv = w % c.Hkv, b = w / c.Hkv;
     const int len = max(c.len(b), 0);
@@ -137,8 +170,9 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
         const int tok = last / a.N > row0 / a.N ? a.N - 1 : last % a.N;      // the block's last token of any head
         seen = min(len, max(0, len - a.N + 1 + tok));
     }
-    const int np = (seen + 63) >> 6, j0 = (int)((long long)np * sp / a.splits), j1 = (int)((long long)np * (sp + 1) / a.splits);
+    const int np = (seen + 63) >> 6, j0 = (int)((long long)np * sp / splits), j1 = (int)((long long)np * (sp + 1) / splits);
     const int n = tiles ? j1 - j0 : 0;
+    const bool alt = C::QT == 2 && tiles == 1;                       // both tiles take these rows, tile h the pages h, h + 2, ..
     if (tid == 0 && item == 0 && kv == 0 && sp == 0 && c.len(b) < 0) c.invalid();
 
     auto fail = [&]() {
@@ -147,16 +181,20 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
     };
     bool ok = true;
 
+    // softmax warps: the thread's row
+    const int h_sm = warp >> 2, r = (warp & 3) * 32 + lane, row = row0 + (alt ? 0 : 128 * h_sm) + r;
+    const bool have = warp < C::SMW && row < rows;
+    const int head = have ? a.units.head[a.units.first[kv] + row / a.N] : 0, tok = have ? row % a.N : 0;
+    float m = -INFINITY, l = 0.f;
+    const int n_tile = alt ? (n + 1 - h_sm) >> 1 : h_sm < tiles ? n : 0;          // pages of the warp's tile
+
     if (warp < C::SMW) {
         // ------------------------------------------------------------------ softmax: a row per thread
-        const int h = warp >> 2, r = (warp & 3) * 32 + lane, row = row0 + 128 * h + r;
+        const int h = h_sm;
         const uint32_t t_w = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_w + h * D, t_s = t_w + C::S_COL + 64 * h,
                        t_p = t_w + C::P_COL + C::P_COLS * h;
-        const bool have = row < rows;
-        const int head = have ? a.units.head[a.units.first[kv] + row / a.N] : 0, tok = have ? row % a.N : 0;
         const int limit = !have ? 0 : a.causal ? len - a.N + 1 + tok : len;
-        float m = -INFINITY, l = 0.f;
-        if (n > 0 && h < tiles) {
+        if (n_tile > 0) {
             const uint16_t* qp = (const uint16_t*)a.q + b * a.qs.b + head * a.qs.h + tok * a.qs.t;
 #pragma unroll 1
             for (int G = 0; G < NG; ++G) {
@@ -210,10 +248,10 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(QF));
-        if (h < tiles) {
+        if (n_tile > 0) {
             const int full = a.causal ? __reduce_min_sync(0xffffffffu, have ? limit : len) : len;      // keys that every row of the warp sees
 #pragma unroll 1
-            for (int j = 0; j < n; ++j) {
+            for (int j = 0; j < n_tile; ++j) {
                 if (!__all_sync(0xffffffffu, tile_wait(bar(SF + h), (uint32_t)j & 1u, &abort_flag))) { fail(); ok = false; break; }
                 tc_fence_after();
                 uint32_t sr[2][32];
@@ -223,9 +261,10 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(SR + h));
-                const int k0 = 64 * (j0 + j);
-                const bool page = there[j & 15];
-                if (k0 + 64 > full || !page) {
+                const int pg = alt ? 2 * j + h : j, k0 = 64 * (j0 + pg);
+                const bool page = there[pg & 15];
+                const bool masked = k0 + 64 > full || !page;
+                if (masked) {
 #pragma unroll
                     for (int i = 0; i < 64; ++i)
                         if (!page || k0 + i >= limit) sr[i >> 5][i & 31] = 0xFF800000u;
@@ -237,6 +276,7 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
                     for (int y = 0; y < 4; ++y)
                         mx[y] = max3(mx[y], __uint_as_float(sr[i >> 5][(i & 31) + 2 * y]), __uint_as_float(sr[i >> 5][(i & 31) + 2 * y + 1]));
                 const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.scale_log2;
+                const bool plain = !masked && __all_sync(0xffffffffu, fabsf(top) < INFINITY);
                 const bool move = top > m + 8.f;
                 float rescale = 1.f;
                 const bool moved = __any_sync(0xffffffffu, move);
@@ -249,18 +289,34 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
                 const float ref = m == -INFINITY ? 0.f : m;
                 const uint64_t c2 = pack2(a.scale_log2, a.scale_log2), r2 = pack2(-ref, -ref);
                 uint64_t sum[2] = {0, 0};
-                // word 4 (2 i + e / 4) + e % 4 of P: tokens 16 i + e and 16 i + 8 + e, the order of the dequantized values
+                float* const x = reinterpret_cast<float*>(&sr[0][0]);
+                // The special-function unit gives 16 exponentials per clk and SM, 1024 clk for the page's: POLY of four pairs go to the
+                // multiply-add pipe, unless a score is masked or not finite (exp2_pair has no zero).
+                auto exponentials = [&](auto poly) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        float p0, p1;
+                        unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), c2, r2), p0, p1);
+                        if (decltype(poly)::value && i % 4 >= 4 - POLY) {
+                            exp2_pair(p0, p1);
+                        } else {
+                            p0 = ex2_approx(p0);
+                            p1 = ex2_approx(p1);
+                        }
+                        sum[i & 1] = add2(sum[i & 1], pack2(p0, p1));
+                        x[2 * i] = p0;
+                        x[2 * i + 1] = p1;
+                    }
+                };
+                if (plain) exponentials(std::true_type{});
+                else exponentials(std::false_type{});
+                // word 8 i + e of P: tokens 16 i + e and 16 i + 8 + e, the order of the dequantized values
                 uint32_t ps[32], pl[32];
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        float p0, p1;
-                        unpack2(fma2(pack2(__uint_as_float(sr[i >> 1][(16 * i + e) & 31]), __uint_as_float(sr[i >> 1][(16 * i + 8 + e) & 31])),
-                                     c2, r2), p0, p1);
-                        p0 = ex2_approx(p0);
-                        p1 = ex2_approx(p1);
-                        sum[e & 1] = add2(sum[e & 1], pack2(p0, p1));
+                        const float p0 = x[16 * i + e], p1 = x[16 * i + 8 + e];
                         const uint32_t hi = Pair16<__nv_bfloat16>::round_pack(p0, p1);
                         ps[8 * i + e] = hi;
                         if (SPLIT) {
@@ -293,40 +349,6 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(PF + h));
-            }
-            // ---- result
-            if (ok && n > 0) {
-                if (!__all_sync(0xffffffffu, tile_wait(bar(OD + h), (uint32_t)(n - 1) & 1u, &abort_flag))) { fail(); ok = false; }
-                tc_fence_after();
-            }
-            if (ok) {
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                const long long part = ((((long long)b * c.Hkv + kv) * a.items + item) * C::QT + h) * a.splits + sp;
-#pragma unroll 1
-                for (int y = 0; y < D; y += 32) {
-                    uint32_t o[32];
-                    if (n > 0) {
-                        tmem_ld32(t_o + y, o);
-                        tmem_wait_ld();
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = 0;
-                    }
-                    if (!have) continue;
-                    if (a.splits == 1) {
-                        const long long at = (((long long)b * a.Hq + head) * a.N + tok) * D + y;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * inv);
-                        tile_store32(a, at, o);
-                    } else {
-                        float4* dst = reinterpret_cast<float4*>(a.part_o + (part * 128 + r) * D + y);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            dst[i] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]),
-                                                 __uint_as_float(o[4 * i + 3]));
-                    }
-                }
-                if (a.splits > 1 && have) a.part_ml[part * 128 + r] = make_float2(m, l);
             }
         }
     } else if (warp < C::W_MMA) {
@@ -389,14 +411,17 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
             constexpr uint32_t ID_S = umma_idesc_bf16(128, 64), ID_O = umma_idesc_bf16(128, D);
             bool good = tile_wait(bar(QF), 0, &abort_flag);
             tc_fence_after();
+            const int behind = alt ? 2 : 1;                          // O += P V of a page goes behind the tile's next S
 #pragma unroll 1
-            for (int j = 0; j <= n && good; ++j) {
-                if (j < n) {                                         // S(j)
+            for (int j = 0; j < n + behind && good; ++j) {
+                if (j < n) {                                         // S of page j, the tile's page jj
+                    const bool mine = alt ? (j & 1) == h : h < tiles;
+                    const int jj = alt ? j >> 1 : j;
                     good = tile_wait(bar(KF + j % C::KS), (uint32_t)(j / C::KS) & 1u, &abort_flag) &&
-                           (j == 0 || h >= tiles || tile_wait(bar(SR + h), (uint32_t)(j - 1) & 1u, &abort_flag));
+                           (!mine || jj == 0 || tile_wait(bar(SR + h), (uint32_t)(jj - 1) & 1u, &abort_flag));
                     if (!good) break;
                     tc_fence_after();
-                    if (h < tiles) {
+                    if (mine) {
                         const uint32_t kl = umma_desc_lo(smem + (j % C::KS) * C::K_STAGE), d = tmem + C::S_COL + 64 * h;
 #pragma unroll
                         for (int term = 0; term < C::TERMS; ++term) {
@@ -416,23 +441,24 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
                         umma_commit(bar(SF + h));
                         umma_commit(bar(KE + j % C::KS));
                     } else {
-                        mbar_arrive(bar(KE + j % C::KS));            // a tile without rows holds nothing up
+                        mbar_arrive(bar(KE + j % C::KS));            // a page that is not this tile's
                     }
                 }
-                if (j > 0) {                                         // O += P(j - 1) V(j - 1)
-                    const int i = j - 1;
+                if (j >= behind) {                                   // O += P V of page i
+                    const int i = j - behind, ii = alt ? i >> 1 : i;
+                    const bool mine = alt ? (i & 1) == h : h < tiles;
                     good = tile_wait(bar(VF + i % C::KS), (uint32_t)(i / C::KS) & 1u, &abort_flag) &&
-                           (h >= tiles || tile_wait(bar(PF + h), (uint32_t)i & 1u, &abort_flag));
+                           (!mine || tile_wait(bar(PF + h), (uint32_t)ii & 1u, &abort_flag));
                     if (!good) break;
                     tc_fence_after();
-                    if (h < tiles) {
+                    if (mine) {
                         const uint32_t vl = umma_desc_lo(smem + C::V_OFF + (i % C::KS) * C::V_STAGE);
 #pragma unroll
                         for (int term = 0; term < C::TERMS; ++term)
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
                                 umma_bf16_ts_lo(tmem + h * D, tmem + C::P_COL + C::P_COLS * h + term * 32 + 8 * k, vl + 2 * k, ID_O,
-                                                i > 0 || term + k > 0);
+                                                ii > 0 || term + k > 0);
                         umma_commit(bar(OD + h));
                         umma_commit(bar(VE + i % C::KS));
                     } else {
@@ -469,6 +495,68 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
     }
     if (!ok) let_copies_land();
     tc_fence_before();
+    __syncthreads();                                                 // every product is complete (the issuers waited for their last ones)
+    tc_fence_after();
+    const bool good = abort_flag == 0;
+    const uint32_t t_o = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (h_sm & 1) * D;
+    // O of the other tile, its reference and sum: [d + 2][128] floats over the K and V tiles
+    float* const other = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)));
+    if (alt) {
+        if (good && warp < C::SMW && h_sm == 1) {
+            other[D * 128 + r] = m;
+            other[(D + 1) * 128 + r] = l;
+            if (n_tile > 0) {
+#pragma unroll 1
+                for (int y = 0; y < D; y += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(t_o + y, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) other[(y + i) * 128 + r] = __uint_as_float(o[i]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (good && warp < (alt ? 4 : 4 * tiles)) {
+        float f0 = 1.f, f1 = 0.f;
+        if (alt) {
+            const float m1 = other[D * 128 + r], M = fmaxf(m, m1);
+            f0 = m == -INFINITY ? 0.f : ex2_approx(m - M);
+            f1 = m1 == -INFINITY ? 0.f : ex2_approx(m1 - M);
+            l = l * f0 + other[(D + 1) * 128 + r] * f1;
+            m = M;
+        }
+        const float inv = splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+        const long long part = ((long long)slot * C::QT + h_sm) * a.splits + sp;
+#pragma unroll 1
+        for (int y = 0; y < D; y += 32) {
+            uint32_t o[32];
+            if (n_tile > 0) {
+                tmem_ld32(t_o + y, o);
+                tmem_wait_ld();
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = 0;
+            }
+            if (alt && n > 1) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + other[(y + i) * 128 + r] * f1);
+            }
+            if (!have) continue;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * inv);
+            if (splits == 1) {
+                tile_store32(a, (((long long)b * a.Hq + head) * a.N + tok) * D + y, o);
+            } else {
+                uint4* dst = reinterpret_cast<uint4*>(a.part_o + (part * 128 + r) * D + y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            }
+        }
+        if (splits > 1 && have) a.part_ml[part * 128 + r] = make_float2(m, l);
+    }
+    tc_fence_before();
     __syncthreads();
     if (warp == C::W_MMA) tmem_dealloc(tmem, 512);
 }
@@ -482,14 +570,14 @@ cache_attention_join_kernel(const __grid_constant__ TileArgs a, int QT)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const long long row_id = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int r = (int)(row_id % (128 * QT));
-    long long w = row_id / (128 * QT);
-    const int item = (int)(w % a.items); w /= a.items;
-    const int kv = (int)(w % a.cache.Hkv), b = (int)(w / a.cache.Hkv);
+    const int r = (int)(row_id % (128 * QT)), slot = (int)(row_id / (128 * QT));
+    int w = a.full + slot;
+    const int item = a.items - 1 - w % a.items; w /= a.items;
+    const int kv = w % a.cache.Hkv, b = w / a.cache.Hkv;
     const int first = a.units.first[kv], rows = (a.units.first[kv + 1] - first) * a.N, row = item * 128 * QT + r;
     if (row >= rows) return;
     const int head = a.units.head[first + row / a.N], tok = row % a.N;
-    const long long p0 = ((((long long)b * a.cache.Hkv + kv) * a.items + item) * QT + r / 128) * a.splits;
+    const long long p0 = ((long long)slot * QT + r / 128) * a.splits;
     const int rr = r % 128;
     float M = -INFINITY, L = 0.f, o[D / 32];
     for (int x = 0; x < a.splits; ++x) M = fmaxf(M, a.part_ml[(p0 + x) * 128 + rr].x);
@@ -520,10 +608,10 @@ static cudaError_t tile_d(const TileArgs& a, cudaStream_t st)
     using C = TileCfg<D, __is_same(T, __half)>;
     static SmemOptIn opt;
     if (!opt.ensure(cache_attention_kernel<T, D>, C::SMEM)) return cudaErrorInvalidValue;
-    const unsigned blocks = (unsigned)(a.cache.B * a.cache.Hkv * a.items);
-    const cudaError_t e = launch_dependent(cache_attention_kernel<T, D>, blocks * (unsigned)a.splits, C::THREADS, C::SMEM, st, a);
-    if (e != cudaSuccess || a.splits == 1) return e;
-    return launch_dependent(cache_attention_join_kernel<D>, blocks * (16 * C::QT), 256, 0, st, a, C::QT);
+    const unsigned blocks = (unsigned)(a.cache.B * a.cache.Hkv * a.items), split = blocks - (unsigned)a.full;
+    const cudaError_t e = launch_dependent(cache_attention_kernel<T, D>, (unsigned)a.full + split * (unsigned)a.splits, C::THREADS, C::SMEM, st, a);
+    if (e != cudaSuccess || split == 0) return e;
+    return launch_dependent(cache_attention_join_kernel<D>, split * (16 * C::QT), 256, 0, st, a, C::QT);
 }
 
 int attention_tile_rows(int dtype, int d) { return 128 * (d == 64 || (d == 128 && dtype == HIFA4_BF16) ? 2 : 1); }
