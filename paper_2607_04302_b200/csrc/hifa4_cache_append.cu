@@ -13,32 +13,37 @@ __device__ __forceinline__ uint32_t nibbles4(const float* y)
     return n | (n >> 4);
 }
 
-// Largest magnitude of a lane's 16 values (packed pairs), of its group of four lanes; a NaN loses.
-template <typename T> __device__ __forceinline__ float group_max(const uint32_t (&x)[8])
+// Largest magnitude of a group, of which each of four lanes has 16 values (packed pairs).  NAN_WINS: a NaN if there is one, else
+// NaN are passed over.
+template <typename T, bool NAN_WINS> __device__ __forceinline__ float group_max(const uint32_t (&x)[8])
 {
+    auto max2 = [](uint32_t a, uint32_t b) { return NAN_WINS ? max16_nan<T>(a, b) : max16<T>(a, b); };
     uint32_t m[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m[i] = max16<T>(abs16<T>(x[i]), abs16<T>(x[i + 4]));
-    m[0] = max16<T>(max16<T>(m[0], m[1]), max16<T>(m[2], m[3]));
-    m[0] = max16<T>(m[0], __shfl_xor_sync(0xffffffffu, m[0], 1));
-    m[0] = max16<T>(m[0], __shfl_xor_sync(0xffffffffu, m[0], 2));
+    for (int i = 0; i < 4; ++i) m[i] = max2(abs16<T>(x[i]), abs16<T>(x[i + 4]));
+    m[0] = max2(max2(m[0], m[1]), max2(m[2], m[3]));
+    m[0] = max2(m[0], __shfl_xor_sync(0xffffffffu, m[0], 1));
+    m[0] = max2(m[0], __shfl_xor_sync(0xffffffffu, m[0], 2));
+    m[0] = max2(m[0], __byte_perm(m[0], m[0], 0x1032));
     float a, b;
     Pair16<T>::unpack(m[0], a, b);
-    return fmaxf(fmaxf(a, b), 0.f);                                          // (a NaN against a NaN)
+    return a;
 }
 
-// A lane's 16 consecutive values (two units) of a group whose largest magnitude is A: nibbles of the four subgroups (nibbles4) and
-// their shifts.  What lies above the E6M2 range saturates, a NaN becomes zero.
-template <typename T>
-__device__ __forceinline__ void quantize16(const uint32_t (&xw)[8], float A, const Hif4Group& g, uint32_t (&nib)[4], int (&k)[4])
+// A lane's 16 consecutive values (two units) of a group: nibbles of the four subgroups (nibbles4) and their shifts.
+// GENERAL: what lies above the E6M2 range saturates, a NaN becomes zero; otherwise there are none.
+template <typename T, bool GENERAL>
+__device__ __forceinline__ void quantize16(const uint32_t (&xw)[8], const Hif4Group& g, uint32_t (&nib)[4], int (&k)[4])
 {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         float x[8], y[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) Pair16<T>::unpack(xw[4 * u + i], x[2 * i], x[2 * i + 1]);
+        if (GENERAL) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -g.top), g.top) : 0.f;
+            for (int i = 0; i < 8; ++i) x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -g.top), g.top) : 0.f;
+        }
         const float a0 = fmaxf(max3(fabsf(x[0]), fabsf(x[1]), fabsf(x[2])), fabsf(x[3]));
         const float a1 = fmaxf(max3(fabsf(x[4]), fabsf(x[5]), fabsf(x[6])), fabsf(x[7]));
         uint32_t w[4];
@@ -47,6 +52,20 @@ __device__ __forceinline__ void quantize16(const uint32_t (&xw)[8], float A, con
         nib[2 * u] = nibbles4(y);
         nib[2 * u + 1] = nibbles4(y + 4);
     }
+}
+// The same from the values alone; *code: the group's scale.  Whole warp: the general form runs where a group of the warp needs it.
+template <typename T> __device__ __forceinline__ void quantize_group(const uint32_t (&xw)[8], uint32_t (&nib)[4], int (&k)[4], int* code)
+{
+    const float A = group_max<T, true>(xw);
+    Hif4Group g = hif4_group(A);
+    if (__any_sync(0xffffffffu, !(A <= g.top))) {
+        float B = group_max<T, false>(xw);
+        g = hif4_group(B == B ? B : 0.f);                                    // (only NaN: zeros)
+        quantize16<T, true>(xw, g, nib, k);
+    } else {
+        quantize16<T, false>(xw, g, nib, k);
+    }
+    *code = g.code;
 }
 
 // One CTA per (sequence, KV head, page that the new tokens touch); four lanes per 64-element group, 16 elements each, which
@@ -132,11 +151,9 @@ cache_append_kernel(const CacheView c, int n, const int* __restrict__ n_new, con
                 xw[2 * e + 1] = Pair16<T>::round_pack(x0 * fe.z, x1 * fe.w);
             }
         }
-        const float A = group_max<T>(xw);
-        const Hif4Group g = hif4_group(A);
         uint32_t nib[4];
-        int sh[4];
-        quantize16<T>(xw, A, g, nib, sh);
+        int sh[4], code;
+        quantize_group<T>(xw, nib, sh, &code);
         uint32_t s = (uint32_t)(sh[0] | sh[1] << 16 | sh[2] << 2 | sh[3] << 18) << (4 * j);
         s |= __shfl_xor_sync(0xffffffffu, s, 1);
         s |= __shfl_xor_sync(0xffffffffu, s, 2);
@@ -145,7 +162,7 @@ cache_append_kernel(const CacheView c, int n, const int* __restrict__ n_new, con
             make_uint2(__byte_perm(nib[0], nib[1], 0x6420), __byte_perm(nib[2], nib[3], 0x6420));
         if (j == 0) {
             *reinterpret_cast<uint32_t*>(pg + P::K_SHIFTS + 4 * (r * NG + G)) = s;
-            pg[P::K_SCALES + r * NG + G] = (uint8_t)g.code;
+            pg[P::K_SCALES + r * NG + G] = (uint8_t)code;
         }
     }
     uint8_t* vp = pg + P::HALF;
@@ -168,11 +185,9 @@ cache_append_kernel(const CacheView c, int n, const int* __restrict__ n_new, con
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const uint32_t (&xw)[8] = x ? xb : xa;
-            const float A = group_max<T>(xw);
-            const Hif4Group g = hif4_group(A);
             uint32_t nib[4];
-            int sh[4];
-            quantize16<T>(xw, A, g, nib, sh);                                // subgroups: tokens 16 j + 4 i + (0..3); word h: i = h and h + 2
+            int sh[4], code;
+            quantize_group<T>(xw, nib, sh, &code);                             // subgroups: tokens 16 j + 4 i + (0..3); word h: i = h and h + 2
             uint32_t s = (uint32_t)(sh[0] | sh[1] << 2 | sh[2] << 16 | sh[3] << 18) << (4 * j);
             s |= __shfl_xor_sync(0xffffffffu, s, 1);
             s |= __shfl_xor_sync(0xffffffffu, s, 2);
@@ -181,7 +196,7 @@ cache_append_kernel(const CacheView c, int n, const int* __restrict__ n_new, con
                 make_uint2(__byte_perm(nib[0], nib[2], 0x6420), __byte_perm(nib[1], nib[3], 0x6420));
             if (j == 0) {
                 *reinterpret_cast<uint32_t*>(vp + P::K_SHIFTS + 4 * ch) = s;
-                vp[P::K_SCALES + ch] = (uint8_t)g.code;
+                vp[P::K_SCALES + ch] = (uint8_t)code;
             }
         }
     }
