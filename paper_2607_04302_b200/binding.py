@@ -525,6 +525,7 @@ class PagedCache:
     def struct(self, in_dtype) -> _Cache:
         st = self._st[in_dtype]
         assert st.pages == self.pages.data_ptr() and (self.v_tail is None or st.v_tail == self.v_tail.data_ptr())
+        assert _here(self.pages)
         return st
 
 
@@ -541,12 +542,17 @@ def alloc_cache(n_pages, Hkv, d, dtype, device, n_tails) -> PagedCache:
                       torch.zeros((n_tails, Hkv, PAGE_TOKENS, d), dtype=dtype, device=device))
 
 
+# The kernels run on the current device (see _stream), so every tensor has to be there: get_device() is its index, -1 on the host.
+def _here(t):
+    return t.get_device() == torch._C._cuda_getDevice()
+
+
 def _ints_ok(t, shape):
-    return t is None or (t.dtype is torch.int32 and t.shape == shape and t.is_cuda and t.is_contiguous())
+    return t is None or (t.dtype is torch.int32 and t.shape == shape and _here(t) and t.is_contiguous())
 
 
 def _floats_ok(t, shape):
-    return t is None or (t.dtype is torch.float32 and t.shape == shape and t.is_cuda and t.is_contiguous())
+    return t is None or (t.dtype is torch.float32 and t.shape == shape and _here(t) and t.is_contiguous())
 
 
 def _seqs(block_table, kv_lens, tail_slots=None) -> _Seqs:
@@ -557,7 +563,7 @@ def _seqs(block_table, kv_lens, tail_slots=None) -> _Seqs:
 
 def _strides(t):
     """Reference to the strides of [B,H,n,d] or [B,H,d] (channels contiguous), None where all is contiguous."""
-    assert t.is_cuda
+    assert _here(t)
     if t.is_contiguous():
         return None
     assert t.stride(-1) == 1
@@ -589,7 +595,7 @@ def cache_read(cache: PagedCache, block_table, kv_lens, n, start=None, out_dtype
         out = [cache.pages.new_empty(shape, dtype=_TORCH_DT[out_dtype]) for _ in range(2)]
     k, v = out
     assert k.is_contiguous() and v.is_contiguous() and tuple(k.shape) == shape == tuple(v.shape) and k.dtype == v.dtype
-    assert _ints_ok(start, (B,))
+    assert _here(k) and _here(v) and _ints_ok(start, (B,))
     sq = _seqs(block_table, kv_lens)
     rc = lib().hifa4_cache_read(C.byref(st), C.byref(sq), n, _ptr(start), _DT[k.dtype], _ptr(k), _ptr(v), _ptr(d_status), _stream())
     _check(rc, "hifa4_cache_read")
@@ -628,7 +634,7 @@ def cache_decode(q, cache: PagedCache, block_table, kv_lens, s=None, out=None, l
     assert _floats_ok(page_weight, shape) and _floats_ok(page_weight_out, shape)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    assert out.is_cuda and out.is_contiguous() and out.shape == q.shape
+    assert _here(out) and out.is_contiguous() and out.shape == q.shape and (workspace is None or _here(workspace))
     if workspace is None:
         workspace = q.new_empty(_cache_workspace_bytes("decode", st.Hkv, d, dt, B, sq.max_pages, Hq, 1, _tuple(q_to_kv),
                                                        page_weight_out is not None), dtype=torch.uint8)
@@ -657,7 +663,7 @@ def cache_attention(q, cache: PagedCache, block_table, kv_lens, causal, s=None, 
     assert d == st.d and B == sq.B and _floats_ok(s, (st.Hkv, d))
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    assert out.is_cuda and out.is_contiguous() and out.shape == q.shape
+    assert _here(out) and out.is_contiguous() and out.shape == q.shape and (workspace is None or _here(workspace))
     if workspace is None:
         workspace = q.new_empty(_cache_workspace_bytes("attention", st.Hkv, d, dt, B, sq.max_pages, Hq, N, _tuple(q_to_kv), False),
                                 dtype=torch.uint8)

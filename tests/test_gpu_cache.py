@@ -393,3 +393,127 @@ def test_captured_step_is_replayed_with_other_lengths():
         torch.cuda.synchronize()
         r = ref.attend(q.cpu()[:, :, None], cache.pages.cpu(), table.cpu(), kv.tolist(), s.cpu())
         check_attention(out[:, :, None], r, d)
+
+
+def test_many_short_sequences():
+    """More sequences than a warp or a block looks over at once; empty ones among them; page weights."""
+    rng = random.Random(5)
+    lens = [rng.choice([0, 1, 63, 64, 65, rng.randint(1, 200)]) for _ in range(301)]
+    cache, table, k, v, s, inv_s = make_cache(lens, 2, 64, "fp16")
+    q = torch.randn((len(lens), 6, 64), generator=torch.Generator().manual_seed(8)).half()
+    w = torch.zeros(table.shape, device=DEV)
+    out = hb().cache_decode(q.to(DEV), cache, table, ints(lens), s=s, page_weight_out=w)
+    r = ref.attend(q[:, :, None], cache.pages.cpu(), table.cpu(), lens, s.cpu())
+    check_attention(out[:, :, None], r, 64)
+    assert torch.allclose(w.double().cpu(), r.weight, rtol=1e-4, atol=1e-6)
+    out = hb().cache_attention(q[:40, :, None].repeat(1, 1, 70, 1).to(DEV), cache, table[:40].contiguous(), ints(lens[:40]), False, s=s)
+    r = ref.attend(q[:40, :, None], cache.pages.cpu(), table[:40].cpu(), lens[:40], s.cpu())
+    check_attention(out[:, :, 69:], r, 64)
+    assert torch.equal(out[:, :, 0], out[:, :, 69])
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,N,dtype,causal,lens", [
+    (8, 2, 64, 64, "fp16", True, [1500, 900]), (8, 2, 128, 64, "fp16", False, [2000, 10]), (2, 1, 256, 100, "bf16", True, [1700]),
+    (2, 1, 256, 80, "fp16", False, [1300]), (4, 1, 128, 64, "bf16", True, [2500]), (2, 2, 128, 128, "bf16", False, [64, 65]),
+    (1, 1, 64, 257, "bf16", True, [300]), (32, 2, 128, 16, "bf16", False, [1, 0, 640]), (3, 1, 128, 43, "bf16", True, [43])])
+def test_attention_split_and_paired_tiles(Hq, Hkv, d, N, dtype, causal, lens):
+    """Blocks shared out over their pages, both tiles on the same rows (an odd and an even number of pages, one page), partly empty tiles."""
+    cache, table, k, v, s, inv_s = make_cache(lens, Hkv, d, dtype, seed=N)
+    q = (torch.randn((len(lens), Hq, N, d), generator=torch.Generator().manual_seed(N)) * 2).to(DT[dtype])
+    out = hb().cache_attention(q.to(DEV), cache, table, ints(lens), causal, s=s)
+    r = ref.attend(q, cache.pages.cpu(), table.cpu(), lens, s.cpu(), causal=causal)
+    check_attention(out, r, d, P_BITS[dtype])
+    again = hb().cache_attention(q.to(DEV), cache, table, ints(lens), causal, s=s)
+    assert torch.equal(out, again)
+
+
+def test_attention_options():
+    """A head map, strides, a scale, FP32 output, a dirty workspace; a missing page and a bad length."""
+    Hq, Hkv, d, N, lens = 7, 3, 128, 40, [300, 64, 130]
+    cache, table, k, v, s, inv_s = make_cache(lens, Hkv, d, "bf16")
+    q_to_kv = [2, 0, 1, 2, 2, 0, 2]
+    x = torch.randn((3, N, Hq, 2 * d), generator=torch.Generator().manual_seed(1)).bfloat16().to(DEV)
+    q = x[..., d:].transpose(1, 2)
+    out = torch.empty(3, Hq, N, d, device=DEV)
+    ws = torch.full((hb().cache_attention_workspace_bytes(cache, 3, table.shape[1], Hq, N, q_to_kv=q_to_kv),), 255, dtype=torch.uint8, device=DEV)
+    hb().cache_attention(q, cache, table, ints(lens), True, out=out, softmax_scale=0.3, q_to_kv=q_to_kv, workspace=ws)
+    r = ref.attend(q.cpu(), cache.pages.cpu(), table.cpu(), lens, None, causal=True, q_to_kv=q_to_kv, scale=0.3)
+    check_attention(out, r, d, 8)
+    t, l, status = table.clone(), ints([300, 64, 10 ** 6]), torch.zeros(1, dtype=torch.int32, device=DEV)
+    t[0, 1] = 10 ** 6
+    bad = hb().cache_attention(q, cache, t, l, False, softmax_scale=0.3, q_to_kv=q_to_kv, d_status=status)
+    good = hb().cache_attention(q, cache, table, ints(lens), False, softmax_scale=0.3, q_to_kv=q_to_kv)
+    assert status.item() == 1 and torch.equal(bad[1], good[1]) and (bad[2] == 0).all()
+    r = ref.attend(q[:1].cpu(), cache.pages.cpu(), table[:1, [0, 2, 3, 4]].cpu(), [300 - 64], None, q_to_kv=q_to_kv, scale=0.3)
+    check_attention(bad[:1], r, d, 8)
+
+
+@pytest.mark.parametrize("N", [1, 3, 40])
+def test_not_a_number_stays_in_its_row(N):
+    """A query row with a NaN, or with an infinity, spoils itself only."""
+    lens = [200, 70]
+    cache, table, k, v, s, inv_s = make_cache(lens, 2, 128, "bf16")
+    q = torch.randn((2, 8, N, 128), generator=torch.Generator().manual_seed(4)).bfloat16()
+    call = lambda q: hb().cache_attention(q.to(DEV), cache, table, ints(lens), False).cpu()
+    clean = call(q)
+    q[0, 3, N - 1, 7], q[1, 5, 0, 9] = math.nan, math.inf
+    out = call(q)
+    assert out[0, 3, N - 1].isnan().all() and out[1, 5, 0].isnan().all()
+    spoilt = torch.zeros(2, 8, N, dtype=torch.bool)
+    spoilt[0, 3, N - 1] = spoilt[1, 5, 0] = True
+    assert torch.equal(out[~spoilt], clean[~spoilt])
+
+
+def test_calls_on_two_streams_at_once():
+    """Two streams, a workspace each (torch gives every call its own), the same cache."""
+    lens = [3000, 500]
+    cache, table, k, v, s, inv_s = make_cache(lens, 2, 128, "bf16")
+    q = torch.randn((2, 8, 128), generator=torch.Generator().manual_seed(4)).bfloat16().to(DEV)
+    qn = torch.randn((2, 8, 50, 128), generator=torch.Generator().manual_seed(5)).bfloat16().to(DEV)
+    one, many = hb().cache_decode(q, cache, table, ints(lens)), hb().cache_attention(qn, cache, table, ints(lens), False)
+    kv = ints(lens)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(hb().cache_decode(q, cache, table, kv) if i == 0 else hb().cache_attention(qn, cache, table, kv, False))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, one) for x in got[0]) and all(torch.equal(x, many) for x in got[1])
+
+
+def test_rows_of_other_sequences_stay():
+    """A batch whose last rows are padding: tables of -1, length 0, no new tokens: pages, tails and page weights stay as they were."""
+    lens = [100, 0, 0]
+    cache, table, k, v, s, inv_s = make_cache(lens, 2, 64, "fp16")
+    pages, tail = cache.pages.clone(), cache.v_tail.clone()
+    w = torch.full(table.shape, 0.5, device=DEV)
+    q = torch.randn((3, 4, 64), generator=torch.Generator().manual_seed(4)).half().to(DEV)
+    kn = torch.randn((3, 2, 1, 64), generator=torch.Generator().manual_seed(6)).half().to(DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    hb().cache_append(cache, kn, kn, table, ints([101, 0, 0]), n_new=ints([1, 0, 0]), d_status=status)
+    hb().cache_decode(q, cache, table, ints([101, 0, 0]), page_weight=w, page_weight_out=w, d_status=status)
+    used = set(table[0, :2].tolist())
+    rest = [p for p in range(pages.shape[0]) if p not in used]
+    assert status.item() == 0 and torch.equal(cache.pages[rest], pages[rest]) and torch.equal(cache.v_tail[1:], tail[1:])
+    assert torch.equal(cache.v_tail[0, :, :36], tail[0, :, :36]) and torch.equal(cache.v_tail[0, :, 37:], tail[0, :, 37:])
+    assert (w[1:] == 0.5).all() and (w[0, 2:] == 0.5).all() and abs(float(w[0, :2].sum()) - 1.0 - 4) < 1e-4
+
+
+def test_binding_refuses_tensors():
+    cache, table, k, v, s, inv_s = make_cache([100], 2, 64, "fp16")
+    q = torch.randn((1, 4, 64), device=DEV).half()
+    bad = [dict(kv_lens=ints([100]).cpu()), dict(kv_lens=ints([100]).long()), dict(block_table=table.cpu()), dict(s=s.double()), dict(q=q.cpu()),
+           dict(q=q[..., ::2]), dict(q=q.float()), dict(lse=torch.empty(4, device=DEV)), dict(out=torch.empty(1, 4, 32, device=DEV)),
+           dict(page_weight_out=torch.zeros(1, 1, device=DEV))]
+    for b in bad:
+        args = dict(q=q, cache=cache, block_table=table, kv_lens=ints([100]), s=s)
+        args.update(b)
+        with pytest.raises((AssertionError, KeyError)):
+            hb().cache_decode(**args)
+    with pytest.raises(AssertionError):
+        hb().cache_append(hb().PagedCache(cache.pages, None), k.to(DEV), v.to(DEV), table, ints([100]))
+    with pytest.raises(hb().Hifa4Error):
+        hb().cache_decode(q, cache, table, ints([100]), workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+    with pytest.raises(hb().Hifa4Error):
+        hb().cache_evict(table, ints([100]), torch.zeros(table.shape, device=DEV), 1, 1, 1)
