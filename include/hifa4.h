@@ -413,9 +413,9 @@ int hifa4_cache_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const h
                        float* page_weight_out, void* workspace, size_t workspace_bytes, int* d_status, void* stream);
 
 /* The same for N >= 1 query tokens per sequence: q [B,Hq,N,d], out [B,Hq,N,d].  Cross attention to an encoder's states of other
- * lengths (causal 0), the next chunk of a prompt or several drafted tokens (causal 1, after their append).  More than 32 query rows
- * (heads times tokens) per KV head take a kernel on tcgen05 in which P is rounded to BF16, for FP16 activations to two terms of
- * BF16 (16 bits).  The workspace may be used by the next call on the same stream. */
+ * lengths (causal 0), the next chunk of a prompt or several drafted tokens (causal 1, after their append).  More than 16 query rows
+ * (heads times tokens; d = 256: 8) per KV head take a kernel on tcgen05 in which P is rounded to BF16, for FP16 activations to two
+ * terms of BF16 (16 bits).  The workspace may be used by the next call on the same stream. */
 size_t hifa4_cache_attention_workspace_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query);
 int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
                           const hifa4_strides* q_strides, const float* s, void* out, void* workspace, size_t workspace_bytes,

@@ -201,7 +201,12 @@ struct TileLayout {
     }
 };
 
-bool tile_kernel_faster(int rows) { return rows > 32; }
+// Rows per KV head from which the tensor-memory kernel is the faster one (us, decode kernel and it; 32 / 8 heads, d = 128, BF16): 8
+// sequences of 4096, 8 rows 22.4 and 38.7, 16 31.7 and 39.5, 32 47.4 and 40.2, 128 138 and 46; 32 of 2048, 16 rows 54 and 66, 32 86
+// and 68; one of 16384, 16 rows 24.5 and 26.4, 32 31.8 and 27.2; FP16, 16 of 1000, 16 rows 25.5 and 23.5; d = 64, FP16, 4 of
+// 1500, 8 rows 10.9 and 13.6, 16 14.4 and 13.6.  d = 256, whose decode kernel takes 8 rows at a time: 8 of 4096, 8 rows 41 and 55, 16
+// 65 and 56.
+bool tile_kernel_faster(int d, int rows) { return rows > (d == 256 ? 8 : 16); }
 
 // Workspace of a call; 0 where it is not built.
 size_t attend_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query, bool weight, bool many)
@@ -210,7 +215,7 @@ size_t attend_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_
     int rows;
     if (!cache || cache->Hkv <= 0 || cache->Hkv > HIFA4_MAX_HEADS || !built(cache->d) || B <= 0 || max_pages <= 0) return 0;
     if (check_query(cache, query, &units, &rows)) return 0;
-    if (many && tile_kernel_faster(rows)) {
+    if (many && tile_kernel_faster(cache->d, rows)) {
         const size_t n = TileLayout(cache, B, max_pages, rows).total;
         return n ? n : 256;
     }
@@ -290,7 +295,7 @@ int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, cons
     Strides qs;
     int rc = check_call(cache, seqs, query, q, q_strides, out, &units, &rows, &qs);
     if (rc) return rc;
-    if (!tile_kernel_faster(rows))
+    if (!tile_kernel_faster(cache->d, rows))
         return run_decode(cache, seqs, query, units, rows, qs, q, s, out, nullptr, nullptr, nullptr, workspace, workspace_bytes, d_status, stream);
     const TileLayout lay(cache, seqs->B, seqs->max_pages, rows);
     if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;

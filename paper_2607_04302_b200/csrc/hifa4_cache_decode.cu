@@ -274,6 +274,9 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
     __shared__ int scratch[W + 1];
     __shared__ Cursor begin_of[W + 1];                 // first page of a consumer's range
     __shared__ int first_page[W + 1];                  // its index among all pages
+    __shared__ volatile int now[W][6];                 // what a consumer does not hold in registers while it goes through pages: the
+                                                       // present segment (Cursor), its first step, the pages left
+    __shared__ volatile int plan[4];                   // steps in all, CTAs, this CTA's first step and the one behind its last
     __shared__ volatile int page_there[W];             // whether the page in a consumer's buffers exists
     __shared__ volatile int gave_up;
     __shared__ Cursor piece[2 * W];                    // pieces of segments that a consumer shares with others: [2 w] begun before it,
@@ -299,22 +302,25 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
     }
     const Shares of_ctas(total, ctas);
     const int cta0 = of_ctas.begin(blockIdx.x), cta1 = of_ctas.begin(blockIdx.x + 1);
-    Cursor cur;
-    int seg_at;                                        // the present segment's first step
     QueryLoad<D, NT> ql;
     {
         const Shares of_warps(cta1 - cta0, W);
         const int w0 = cta0 + of_warps.begin(warp);    // warp W: where the next CTA begins
-        int index;
-        cur = locate(c, U, min(w0, total - 1), lane, &index, &seg_at);
+        int index, seg_at;
+        const Cursor cur = locate(c, U, min(w0, total - 1), lane, &index, &seg_at);
         if (warp < W && cur.np > 0) ql.template issue<ROWS>(a, cur, g, t);      // ahead of the flood of page loads
         if (lane == 0) {
             begin_of[warp] = cur;
             first_page[warp] = index;
+            if (warp < W) {
+                now[warp][0] = cur.b; now[warp][1] = cur.u; now[warp][2] = cur.p; now[warp][3] = cur.np; now[warp][4] = seg_at;
+            }
         }
+        if (tid == 0) { plan[0] = total; plan[1] = ctas; plan[2] = cta0; plan[3] = cta1; }
     }
     __syncthreads();
-    int remaining = warp < W ? first_page[warp + 1] - first_page[warp] : 0;
+    if (warp < W && lane == 0) now[warp][5] = first_page[warp + 1] - first_page[warp];
+    __syncwarp();
     if (warp == W) {
         // ---- loads: lane i feeds consumer i, a half page at a time, whenever the consumer has read the one before
         if (lane < W) {
@@ -356,8 +362,9 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
     uint32_t phase = 0;
     bool ok = true;
 #pragma unroll 1
-    while (remaining > 0 && ok) {
+    while (warp < W && now[warp][5] > 0) {
         // ---- a segment: query operands
+        Cursor cur{now[warp][0], now[warp][1], now[warp][2], now[warp][3]};
         const int kv = kv_of(a, cur.u), len = c.len(cur.b);
         float f_log2[NT][2];                           // what makes a product a score times log2(e), columns 2t, 2t + 1
         int stat_row[NT][2];                           // (sequence, query head) of columns 2t, 2t + 1, -1: no such row
@@ -449,10 +456,9 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[j][nt][e] = 0.f;
         }
-        const int first_p = cur.p, n_here = min(cur.np - cur.p, remaining);
+        const int end_p = min(cur.np, cur.p + now[warp][5]);
 #pragma unroll 1
-        for (int pi = 0; pi < n_here; ++pi) {
-            const int p = first_p + pi;
+        for (int p = cur.p; p < end_p; ++p) {
             // ---- S = K q~
             if (!__all_sync(0xffffffffu, mbar_wait(bars, phase))) { ok = false; break; }
             const bool there = page_there[warp];
@@ -627,10 +633,11 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
             for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], x);
-        remaining -= n_here;
-        const bool begins = first_p == 0, ends = first_p + n_here == cur.np;
+        cur = Cursor{now[warp][0], now[warp][1], now[warp][2], now[warp][3]};
+        const int seg_at = now[warp][4], remaining = now[warp][5] - (end_p - cur.p);
+        const bool begins = cur.p == 0, ends = end_p == cur.np;
         if (begins && a.seg_ctas && lane == 0)                      // for the page weights: the CTAs that hold the segment
-            a.seg_ctas[(long long)cur.b * U + cur.u] = make_int2(blockIdx.x, Shares(total, ctas).owner(seg_at + 2 * cur.np - 1));
+            a.seg_ctas[(long long)cur.b * units_per_seq(a) + cur.u] = make_int2(blockIdx.x, Shares(plan[0], plan[1]).owner(seg_at + 2 * cur.np - 1));
         if (begins && ends) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -673,15 +680,21 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
             }
         }
         // next segment
-        seg_at += steps_of(cur.np);
+        const int next_at = seg_at + steps_of(cur.np);
         cur.p = 0;
         if (ends && remaining > 0) {
+            const int U = units_per_seq(a);
             if (++cur.u == U) {
                 cur.u = 0;
                 do { ++cur.b; } while (cur.b < c.B && (cur.np = c.n_pages_of(cur.b)) == 0);
             }
             ql.template issue<ROWS>(a, cur, g, t);
         }
+        __syncwarp();                                               // (every lane has read)
+        if (lane == 0) {
+            now[warp][0] = cur.b; now[warp][1] = cur.u; now[warp][2] = 0; now[warp][3] = cur.np; now[warp][4] = next_at; now[warp][5] = remaining;
+        }
+        __syncwarp();
     }
     if (!ok) {
         gave_up = 1;
@@ -690,16 +703,16 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
     }
     // ---- pieces that warps share: a row of a segment per warp and turn
     __syncthreads();
-    const int at = lane < 2 * W ? piece_at[lane] : -1;
+    const int at = lane < 2 * W ? piece_at[lane] : -1, cta_first = plan[2], cta_end = plan[3];
     const bool second = lane & 1;
-    const unsigned first = __ballot_sync(0xffffffffu, !second && at >= 0 && at + 1 < cta0);      // of the segment that a CTA before began
+    const unsigned first = __ballot_sync(0xffffffffu, !second && at >= 0 && at + 1 < cta_first);      // of the segment that a CTA before began
     unsigned leaders = __ballot_sync(0xffffffffu, second && at >= 0) | (first & (0u - first));
-    const unsigned cross = __ballot_sync(0xffffffffu, second && at >= 0 && at + 2 * piece[lane].np - 1 >= cta1);
+    const unsigned cross = __ballot_sync(0xffffffffu, second && at >= 0 && at + 2 * piece[lane].np - 1 >= cta_end);
     if (tid == 0) {                                                  // what the join finds here
         int4 x = make_int4(-1, 0, 0, 0);
         if (cross) {
             const Cursor sg = piece[__ffs(cross) - 1];
-            x = make_int4(sg.b, sg.u, Shares(total, ctas).owner(piece_at[__ffs(cross) - 1] + 2 * sg.np - 1), 0);
+            x = make_int4(sg.b, sg.u, Shares(plan[0], plan[1]).owner(piece_at[__ffs(cross) - 1] + 2 * sg.np - 1), 0);
         }
         a.begun[blockIdx.x] = x;
     }
@@ -710,7 +723,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
         const int seg = __shfl_sync(0xffffffffu, at, lead);
         const unsigned members = __ballot_sync(0xffffffffu, !second && at == seg) | (1u << lead);
         const Cursor sg = piece[lead];
-        const bool begun_here = seg + 1 >= cta0, whole = begun_here && seg + 2 * sg.np - 1 < cta1, mine = members >> lane & 1;
+        const bool begun_here = seg + 1 >= cta_first, whole = begun_here && seg + 2 * sg.np - 1 < cta_end, mine = members >> lane & 1;
         const int ws = 2 * (int)blockIdx.x + (begun_here ? 1 : 0);
         const int kv = kv_of(a, sg.u), rows = min(ROWS, (a.units.first[kv + 1] - a.units.first[kv]) * a.N - (sg.u - kv * a.blocks) * ROWS);
 #pragma unroll 1
