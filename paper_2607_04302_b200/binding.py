@@ -522,10 +522,10 @@ class PagedCache:
         make = lambda dt: _Cache(Hkv, nbytes // 74, dt, n_pages, pages.data_ptr(), n_tails, _ptr(tail))
         object.__setattr__(self, "_st", {dt: make(dt) for dt in (F16, BF16)})
 
-    def struct(self, in_dtype) -> _Cache:
-        st = self._st[in_dtype]
-        assert st.pages == self.pages.data_ptr() and (self.v_tail is None or st.v_tail == self.v_tail.data_ptr())
-        assert _here(self.pages)
+    def struct(self, in_dtype, dev=None) -> _Cache:
+        st, pages, tail = self._st[in_dtype], self.pages, self.v_tail
+        assert st.pages == pages.data_ptr() and (tail is None or st.v_tail == tail.data_ptr())
+        assert pages.get_device() == (_get_device() if dev is None else dev)
         return st
 
 
@@ -542,28 +542,28 @@ def alloc_cache(n_pages, Hkv, d, dtype, device, n_tails) -> PagedCache:
                       torch.zeros((n_tails, Hkv, PAGE_TOKENS, d), dtype=dtype, device=device))
 
 
-# The kernels run on the current device (see _stream), so every tensor has to be there: get_device() is its index, -1 on the host.
-def _here(t):
-    return t.get_device() == torch._C._cuda_getDevice()
+# The kernels run on the current device, so every tensor has to be there (get_device() is -1 on the host).  A step of a short dialogue is
+# bound by host time: the checks of a call share what they look up.
+_get_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+_I32, _FP32 = torch.int32, torch.float32
 
 
-def _ints_ok(t, shape):
-    return t is None or (t.dtype is torch.int32 and t.shape == shape and _here(t) and t.is_contiguous())
+def _ok(t, dtype, shape, dev):
+    """A contiguous tensor of this type and shape on device `dev`."""
+    return t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous()
 
 
-def _floats_ok(t, shape):
-    return t is None or (t.dtype is torch.float32 and t.shape == shape and _here(t) and t.is_contiguous())
-
-
-def _seqs(block_table, kv_lens, tail_slots=None) -> _Seqs:
+def _seqs(block_table, kv_lens, dev, tail_slots=None) -> _Seqs:
     shape = B, max_pages = block_table.shape
-    assert _ints_ok(block_table, shape) and _ints_ok(kv_lens, shape[:1]) and _ints_ok(tail_slots, shape[:1])
-    return _Seqs(B, max_pages, block_table.data_ptr(), kv_lens.data_ptr(), _ptr(tail_slots))
+    lens = shape[:1]
+    assert _ok(block_table, _I32, shape, dev) and _ok(kv_lens, _I32, lens, dev)
+    assert tail_slots is None or _ok(tail_slots, _I32, lens, dev)
+    return _Seqs(B, max_pages, block_table.data_ptr(), kv_lens.data_ptr(), None if tail_slots is None else tail_slots.data_ptr())
 
 
-def _strides(t):
+def _strides(t, dev):
     """Reference to the strides of [B,H,n,d] or [B,H,d] (channels contiguous), None where all is contiguous."""
-    assert _here(t)
+    assert t.get_device() == dev
     if t.is_contiguous():
         return None
     assert t.stride(-1) == 1
@@ -574,13 +574,14 @@ def _strides(t):
 def cache_append(cache: PagedCache, k, v, block_table, kv_lens, n_new=None, inv_s=None, tail_slots=None, d_status=None):
     """Smooths and quantizes new keys and values k, v [B,Hkv,n,d] into the cache's pages.  kv_lens [B] counts the new
     tokens; n_new [B]: how many of the n rows a sequence takes (None: all).  int32 device tensors."""
-    B, Hkv, n, d = k.shape
-    st = cache.struct(_DT[k.dtype])
-    assert v.shape == k.shape and v.dtype is k.dtype and Hkv == st.Hkv and d == st.d and block_table.shape[0] == B
-    assert cache.v_tail is not None and cache.v_tail.dtype is k.dtype
-    assert _ints_ok(n_new, (B,)) and _floats_ok(inv_s, (Hkv, d))
-    rc = lib().hifa4_cache_append(C.byref(st), C.byref(_seqs(block_table, kv_lens, tail_slots)), n, _ptr(n_new), k.data_ptr(),
-                                  _strides(k), v.data_ptr(), _strides(v), _ptr(inv_s), _ptr(d_status), _stream())
+    shape = B, Hkv, n, d = k.shape
+    dev, dt = _get_device(), k.dtype
+    st, sq = cache.struct(_DT[dt], dev), _seqs(block_table, kv_lens, dev, tail_slots)
+    assert v.shape == shape and v.dtype is dt and Hkv == st.Hkv and d == st.d and B == sq.B
+    assert cache.v_tail is not None and cache.v_tail.dtype is dt
+    assert (n_new is None or _ok(n_new, _I32, shape[:1], dev)) and (inv_s is None or _ok(inv_s, _FP32, (Hkv, d), dev))
+    rc = lib().hifa4_cache_append(C.byref(st), C.byref(sq), n, _ptr(n_new), k.data_ptr(), _strides(k, dev), v.data_ptr(),
+                                  _strides(v, dev), _ptr(inv_s), _ptr(d_status), _raw_stream(dev))
     if rc:
         _check(rc, "hifa4_cache_append")
 
@@ -588,17 +589,16 @@ def cache_append(cache: PagedCache, k, v, block_table, kv_lens, n_new=None, inv_
 def cache_read(cache: PagedCache, block_table, kv_lens, n, start=None, out_dtype=BF16, out=None, d_status=None):
     """The values in the cache: (k, v) [B,Hkv,n,d], token i of row b at position start[b] + i (None: i).  Rows at or behind
     kv_lens[b] are left as they were (out = (k, v): the caller's tensors)."""
-    st = cache.struct(BF16)
-    B = block_table.shape[0]
-    shape = (B, st.Hkv, n, st.d)
-    if out is None:
-        out = [cache.pages.new_empty(shape, dtype=_TORCH_DT[out_dtype]) for _ in range(2)]
-    k, v = out
-    assert k.is_contiguous() and v.is_contiguous() and tuple(k.shape) == shape == tuple(v.shape) and k.dtype == v.dtype
-    assert _here(k) and _here(v) and _ints_ok(start, (B,))
-    sq = _seqs(block_table, kv_lens)
-    rc = lib().hifa4_cache_read(C.byref(st), C.byref(sq), n, _ptr(start), _DT[k.dtype], _ptr(k), _ptr(v), _ptr(d_status), _stream())
-    _check(rc, "hifa4_cache_read")
+    dev = _get_device()
+    st, sq = cache.struct(BF16, dev), _seqs(block_table, kv_lens, dev)
+    shape = (sq.B, st.Hkv, n, st.d)
+    k, v = out if out is not None else [cache.pages.new_empty(shape, dtype=_TORCH_DT[out_dtype]) for _ in range(2)]
+    dt = k.dtype
+    assert _ok(k, dt, shape, dev) and _ok(v, dt, shape, dev) and (start is None or _ok(start, _I32, shape[:1], dev))
+    rc = lib().hifa4_cache_read(C.byref(st), C.byref(sq), n, _ptr(start), _DT[dt], k.data_ptr(), v.data_ptr(), _ptr(d_status),
+                                _raw_stream(dev))
+    if rc:
+        _check(rc, "hifa4_cache_read")
     return k, v
 
 
@@ -626,22 +626,27 @@ def cache_decode(q, cache: PagedCache, block_table, kv_lens, s=None, out=None, l
                  page_weight_out=None, workspace=None, softmax_scale=0.0, q_to_kv=None, d_status=None):
     """Attention of one new token per sequence, q [B,Hq,d], over the cache -> out [B,Hq,d] (dtype of `out`, or of q).
     lse [B,Hq], page_weight and page_weight_out [B,max_pages]: float32 device tensors, see include/hifa4.h."""
-    B, Hq, d = q.shape
-    dt = _DT[q.dtype]
-    st, sq = cache.struct(dt), _seqs(block_table, kv_lens)
-    shape = block_table.shape
-    assert d == st.d and B == sq.B and _floats_ok(s, (st.Hkv, d)) and _floats_ok(lse, (B, Hq))
-    assert _floats_ok(page_weight, shape) and _floats_ok(page_weight_out, shape)
+    q_shape = B, Hq, d = q.shape
+    dev, dt, shape = _get_device(), _DT[q.dtype], block_table.shape
+    st, sq = cache.struct(dt, dev), _seqs(block_table, kv_lens, dev)
+    assert d == st.d and B == sq.B and (s is None or _ok(s, _FP32, (st.Hkv, d), dev)) and (lse is None or _ok(lse, _FP32, (B, Hq), dev))
+    assert page_weight is None or _ok(page_weight, _FP32, shape, dev)
+    assert page_weight_out is None or _ok(page_weight_out, _FP32, shape, dev)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    assert _here(out) and out.is_contiguous() and out.shape == q.shape and (workspace is None or _here(workspace))
+    else:
+        assert _ok(out, out.dtype, q_shape, dev)
+    if q_to_kv is not None:
+        q_to_kv = _tuple(q_to_kv)
     if workspace is None:
-        workspace = q.new_empty(_cache_workspace_bytes("decode", st.Hkv, d, dt, B, sq.max_pages, Hq, 1, _tuple(q_to_kv),
+        workspace = q.new_empty(_cache_workspace_bytes("decode", st.Hkv, d, dt, B, sq.max_pages, Hq, 1, q_to_kv,
                                                        page_weight_out is not None), dtype=torch.uint8)
+    else:
+        assert workspace.get_device() == dev
     keep, mp = _map_arr(q_to_kv)
     rc = lib().hifa4_cache_decode(C.byref(st), C.byref(sq), C.byref(_CacheQuery(Hq, mp, 1, 0, _DT[out.dtype], softmax_scale)),
-                                  q.data_ptr(), _strides(q), _ptr(s), out.data_ptr(), _ptr(lse), _ptr(page_weight),
-                                  _ptr(page_weight_out), workspace.data_ptr(), workspace.numel(), _ptr(d_status), _stream())
+                                  q.data_ptr(), _strides(q, dev), _ptr(s), out.data_ptr(), _ptr(lse), _ptr(page_weight),
+                                  _ptr(page_weight_out), workspace.data_ptr(), workspace.nbytes, _ptr(d_status), _raw_stream(dev))
     if rc:
         _check(rc, "hifa4_cache_decode")
     return out
@@ -657,20 +662,25 @@ def cache_attention(q, cache: PagedCache, block_table, kv_lens, causal, s=None, 
                     q_to_kv=None, d_status=None):
     """Attention of q [B,Hq,N,d] over the cache: all keys of each sequence (cross attention), or, causal, those up to the
     query's own position when the N queries are the sequence's last N tokens -> out [B,Hq,N,d]."""
-    B, Hq, N, d = q.shape
-    dt = _DT[q.dtype]
-    st, sq = cache.struct(dt), _seqs(block_table, kv_lens)
-    assert d == st.d and B == sq.B and _floats_ok(s, (st.Hkv, d))
+    q_shape = B, Hq, N, d = q.shape
+    dev, dt = _get_device(), _DT[q.dtype]
+    st, sq = cache.struct(dt, dev), _seqs(block_table, kv_lens, dev)
+    assert d == st.d and B == sq.B and (s is None or _ok(s, _FP32, (st.Hkv, d), dev))
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    assert _here(out) and out.is_contiguous() and out.shape == q.shape and (workspace is None or _here(workspace))
+    else:
+        assert _ok(out, out.dtype, q_shape, dev)
+    if q_to_kv is not None:
+        q_to_kv = _tuple(q_to_kv)
     if workspace is None:
-        workspace = q.new_empty(_cache_workspace_bytes("attention", st.Hkv, d, dt, B, sq.max_pages, Hq, N, _tuple(q_to_kv), False),
+        workspace = q.new_empty(_cache_workspace_bytes("attention", st.Hkv, d, dt, B, sq.max_pages, Hq, N, q_to_kv, False),
                                 dtype=torch.uint8)
+    else:
+        assert workspace.get_device() == dev
     keep, mp = _map_arr(q_to_kv)
     rc = lib().hifa4_cache_attention(C.byref(st), C.byref(sq), C.byref(_CacheQuery(Hq, mp, N, causal, _DT[out.dtype], softmax_scale)),
-                                     q.data_ptr(), _strides(q), _ptr(s), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                                     _ptr(d_status), _stream())
+                                     q.data_ptr(), _strides(q, dev), _ptr(s), out.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                                     _ptr(d_status), _raw_stream(dev))
     if rc:
         _check(rc, "hifa4_cache_attention")
     return out
@@ -697,15 +707,16 @@ def cache_evict(block_table, kv_lens, page_weight, keep_pages, keep_first=1, kee
                 d_status=None) -> Evicted:
     """Takes the pages with the least weight out of the block tables of sequences longer than keep_pages pages; the first
     keep_first and the last keep_last stay.  The tensors of `out` may be the inputs."""
-    shape = tuple(block_table.shape)
-    assert page_weight is not None and _floats_ok(page_weight, shape)
-    sq = _seqs(block_table, kv_lens)
+    dev, shape = _get_device(), block_table.shape
+    lens = shape[:1]
+    sq = _seqs(block_table, kv_lens, dev)
     if out is None:
         out = alloc_evicted(block_table)
-    assert _ints_ok(out.block_table, shape) and _ints_ok(out.kv_lens, shape[:1]) and _floats_ok(out.page_weight, shape)
-    assert _ints_ok(out.freed, shape) and _ints_ok(out.n_freed, shape[:1])
-    rc = lib().hifa4_cache_evict(C.byref(sq), _ptr(page_weight), int(keep_pages), int(keep_first), int(keep_last),
-                                 _ptr(out.block_table), _ptr(out.kv_lens), _ptr(out.page_weight), _ptr(out.freed),
-                                 _ptr(out.n_freed), _ptr(d_status), _stream())
-    _check(rc, "hifa4_cache_evict")
+    assert _ok(page_weight, _FP32, shape, dev) and _ok(out.block_table, _I32, shape, dev) and _ok(out.kv_lens, _I32, lens, dev)
+    assert _ok(out.page_weight, _FP32, shape, dev) and _ok(out.freed, _I32, shape, dev) and _ok(out.n_freed, _I32, lens, dev)
+    rc = lib().hifa4_cache_evict(C.byref(sq), page_weight.data_ptr(), keep_pages, keep_first, keep_last, out.block_table.data_ptr(),
+                                 out.kv_lens.data_ptr(), out.page_weight.data_ptr(), out.freed.data_ptr(), out.n_freed.data_ptr(),
+                                 _ptr(d_status), _raw_stream(dev))
+    if rc:
+        _check(rc, "hifa4_cache_evict")
     return out

@@ -68,13 +68,15 @@ int check_query(const hifa4_cache* c, const hifa4_cache_query* q, CacheUnits* un
     HeadMap qmap, kmap;
     const int rc = build_map(q->Hq, c->Hkv, q->q_to_kv, qmap, kmap);
     if (rc) return rc;
-    int at = 0, most = 0;
+    int count[HIFA4_MAX_HEADS + 1] = {0}, most = 0, at = 0;
+    for (int h = 0; h < q->Hq; ++h) ++count[qmap.kv_of[h]];
     for (int g = 0; g < c->Hkv; ++g) {
         units->first[g] = (short)at;
-        for (int h = 0; h < q->Hq; ++h)
-            if (qmap.kv_of[h] == g) units->head[at++] = (uint8_t)h;
-        most = at - units->first[g] > most ? at - units->first[g] : most;
+        at += count[g];
+        most = count[g] > most ? count[g] : most;
+        count[g] = units->first[g];                                  // where the head map's next head goes
     }
+    for (int h = 0; h < q->Hq; ++h) units->head[count[qmap.kv_of[h]]++] = (uint8_t)h;
     units->first[c->Hkv] = (short)at;
     *rows = most * q->N;
     return HIFA4_OK;
