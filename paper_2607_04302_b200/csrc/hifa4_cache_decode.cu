@@ -725,7 +725,8 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
         const Cursor sg = piece[lead];
         const bool begun_here = seg + 1 >= cta_first, whole = begun_here && seg + 2 * sg.np - 1 < cta_end, mine = members >> lane & 1;
         const int ws = 2 * (int)blockIdx.x + (begun_here ? 1 : 0);
-        const int kv = kv_of(a, sg.u), rows = min(ROWS, (a.units.first[kv + 1] - a.units.first[kv]) * a.N - (sg.u - kv * a.blocks) * ROWS);
+        const int kv = kv_of(a, sg.u);                               // (a block of rows that this KV head does not have: none)
+        const int rows = max(0, min(ROWS, (a.units.first[kv + 1] - a.units.first[kv]) * a.N - (sg.u - kv * a.blocks) * ROWS));
 #pragma unroll 1
         for (; turn < rows; turn += W + 1) {
             const int r = turn;

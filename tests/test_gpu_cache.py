@@ -517,3 +517,23 @@ def test_binding_refuses_tensors():
         hb().cache_decode(q, cache, table, ints([100]), workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
     with pytest.raises(hb().Hifa4Error):
         hb().cache_evict(table, ints([100]), torch.zeros(table.shape, device=DEV), 1, 1, 1)
+
+
+@pytest.mark.parametrize("counts", [(17, 0, 3), (1, 9, 0), (0, 0, 5)])
+@pytest.mark.parametrize("N", [1, 2, 24])
+def test_uneven_head_maps(counts, N):
+    """KV heads with very different numbers of query heads, none among them: blocks of rows that do not exist."""
+    q_to_kv = [g for g, n in enumerate(counts) for _ in range(n)]
+    random.Random(1).shuffle(q_to_kv)
+    lens = [900, 64, 0, 321] + [300] * 60
+    cache, table, k, v, s, inv_s = make_cache(lens, 3, 64, "fp16")
+    q = torch.randn((64, len(q_to_kv), N, 64), generator=torch.Generator().manual_seed(2)).half()
+    out = torch.full(q.shape, 9.0, dtype=torch.float16, device=DEV)
+    hb().cache_attention(q.to(DEV), cache, table, ints(lens), False, s=s, q_to_kv=q_to_kv, out=out)
+    r = ref.attend(q, cache.pages.cpu(), table.cpu(), lens, s.cpu(), q_to_kv=q_to_kv)
+    check_attention(out, r, 64)
+    if N == 1:
+        w = torch.zeros(table.shape, device=DEV)
+        one = hb().cache_decode(q[:, :, 0].to(DEV), cache, table, ints(lens), s=s, q_to_kv=q_to_kv, page_weight_out=w)
+        check_attention(one[:, :, None], r, 64)
+        assert torch.allclose(w.double().cpu(), r.weight, rtol=1e-4, atol=1e-6)
