@@ -6,9 +6,11 @@
 // consumer warps of one CTA per SM in contiguous ranges of equal cost, whatever the sequences' lengths: a page costs two steps,
 // beginning a (sequence, block) one (400 of 1500 instructions, and what it stores).  A consumer takes whole pages on
 // its own: it forms S of the page's 64 tokens, its softmax and O, all in registers, without any exchange between
-// warps.  One more warp loads the pages (bulk copies, a lane per consumer).  The pages of one (sequence, block) that a
-// range holds are a piece of its segment; pieces that warps of one CTA share are joined in shared memory, those that CTAs share by
-// a second, small kernel.
+// warps.  At d = 256, where registers leave room for 7 such warps only, a consumer is a pair of warps: each forms S of half the
+// page's tokens and O of half the channels; maxima and P pass through shared memory (8 sequences of 5-8K tokens, 16 / 8 heads:
+// 54 us with single warps, 48.5 with pairs).  One more warp loads the pages (bulk copies, a lane per consumer).  The pages of one
+// (sequence, block) that a range holds are a piece of its segment; pieces that consumers of one CTA share are joined in shared
+// memory, those that CTAs share by a second, small kernel.
 //
 // Products run on mma.sync m16n8k16 with the cache as the 16-row operand, tokens (S) or channels (O) its rows, and query rows as the
 // 8 columns: an operand of 5 or 6 query rows would leave a 128-row tcgen05 tile nearly empty, and its other operand would have to
@@ -93,16 +95,17 @@ __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint3
 }
 __device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
 
-// NT: 8-row column tiles of query rows.  A consumer has room for one page; the K half is loaded again while V is multiplied, and
-// the other way round.  The query operands wait in shared memory while V is multiplied.
+// NT: 8-row column tiles of query rows.  A consumer (a warp, or a pair of them) has room for one page; the K half is loaded again
+// while V is multiplied, and the other way round.  The query operands wait in shared memory while V is multiplied.
 template <int D, int NT> struct DecodeCfg {
     static constexpr int W = D == 256 ? 7 : NT == 1 ? 15 : D == 128 ? 7 : 11;   // consumers
-    static constexpr int THREADS = (W + 1) * 32;
+    static constexpr int PAIR = D == 256 ? 2 : 1;                        // warps of a consumer
+    static constexpr int WARPS = W * PAIR + 1, THREADS = WARPS * 32;
     static constexpr int ROWS = 8 * NT;
     static constexpr int PV_ROW = 36;                                    // words of P per query row: 32 and 4 against bank conflicts
     static constexpr int PIECE = ROWS * (D + 2);                         // floats of a partial result: O [ROWS][D], then (m, l) [ROWS]
     static constexpr int K_OFF = 0, V_OFF = Page<D>::HALF, P_OFF = Page<D>::BYTES, Q_OFF = P_OFF + NT * 8 * PV_ROW * 4;
-    static constexpr int PER_WARP = Q_OFF + ROWS * D * 2;
+    static constexpr int PER_WARP = Q_OFF + PAIR * ROWS * D * 2;
     static constexpr int BAR_OFF = W * PER_WARP;                         // per consumer: K landed, V landed, K read, V read
     static constexpr int SMEM = BAR_OFF + W * 32 + 64;
     static_assert(PER_WARP % 16 == 0 && Page<D>::HALF % 16 == 0 && PIECE * 4 <= PER_WARP && SMEM <= 227 * 1024 - 2048, "shared memory");
@@ -262,19 +265,30 @@ template <int D, int NT> struct QueryLoad {
 // Factor that takes sums under the reference m to the reference M >= m (both -inf: nothing there).
 __device__ __forceinline__ float rebase(float m, float M) { return m == -INFINITY ? 0.f : exp2f(m - M); }
 
+// Both warps of consumer i meet (named barrier i + 1); whether x holds for both: neither waits for one that gave up.
+__device__ __forceinline__ bool pair_sync(int i, bool x)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)x), "r"(i + 1) : "memory");
+    return r != 0;
+}
+
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(DecodeCfg<D, NT>::THREADS, 1)
 cache_decode_kernel(const __grid_constant__ DecodeArgs a)
 {
     using C = DecodeCfg<D, NT>;
     using P = Page<D>;
-    constexpr int NG = P::NG, W = C::W, ROWS = C::ROWS;
+    constexpr int NG = P::NG, W = C::W, ROWS = C::ROWS, PAIR = C::PAIR;
+    static_assert(PAIR == 1 || NT == 1, "a pair exchanges 8 rows");
+    constexpr int TI = 4 / PAIR, CJ = D / 16 / PAIR;   // a warp's 16-token and 16-channel tiles of a page
     constexpr bool BF = sizeof(T) == 2 && !__is_same(T, __half);
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int scratch[W + 1];
+    __shared__ int scratch[C::WARPS];
     __shared__ Cursor begin_of[W + 1];                 // first page of a consumer's range
     __shared__ int first_page[W + 1];                  // its index among all pages
-    __shared__ volatile int now[W][6];                 // what a consumer does not hold in registers while it goes through pages: the
+    __shared__ volatile int now[W * PAIR][6];          // what a warp does not hold in registers while it goes through pages: the
                                                        // present segment (Cursor), its first step, the pages left
     __shared__ volatile int plan[4];                   // steps in all, CTAs, this CTA's first step and the one behind its last
     __shared__ volatile int page_there[W];             // whether the page in a consumer's buffers exists
@@ -283,12 +297,15 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
                                                        // [2 w + 1] in it
     __shared__ int piece_at[2 * W];                    // the segment's first step, -1: no such piece
     __shared__ float* piece_of[2 * W];                 // where it is
+    constexpr int PAIRS = PAIR == 2 ? W : 1;           // what the two warps of a consumer tell each other, per query row
+    __shared__ volatile float pair_max[PAIRS][2][8], pair_sum[PAIRS][2][8], pair_l[PAIRS][2][8];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const uint32_t base = smem_u32(smem) + warp * C::PER_WARP;
-    const uint32_t kb = base + C::K_OFF, vb = base + C::V_OFF, pbuf = base + C::P_OFF, qbuf = base + C::Q_OFF + 16 * lane;
-    const uint32_t bars = smem_u32(smem) + C::BAR_OFF + warp * 32;
-    if (tid < 4 * W) mbar_init(smem_u32(smem) + C::BAR_OFF + 8 * tid, 1);
+    const int cons = warp / PAIR, half = warp % PAIR;  // (the loader: consumer W)
+    const uint32_t base = smem_u32(smem) + cons * C::PER_WARP;
+    const uint32_t kb = base + C::K_OFF, vb = base + C::V_OFF, pbuf = base + C::P_OFF, qbuf = base + C::Q_OFF + half * ROWS * D * 2 + 16 * lane;
+    const uint32_t bars = smem_u32(smem) + C::BAR_OFF + cons * 32;
+    if (tid < 4 * W) mbar_init(smem_u32(smem) + C::BAR_OFF + 8 * tid, tid & 2 ? PAIR : 1);
     if (tid < 2 * W) piece_at[tid] = -1;
     if (tid == 0) gave_up = 0;
     fence_barrier_init();
@@ -305,23 +322,25 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
     QueryLoad<D, NT> ql;
     {
         const Shares of_warps(cta1 - cta0, W);
-        const int w0 = cta0 + of_warps.begin(warp);    // warp W: where the next CTA begins
+        const int w0 = cta0 + of_warps.begin(cons);    // the loader: where the next CTA begins
         int index, seg_at;
         const Cursor cur = locate(c, U, min(w0, total - 1), lane, &index, &seg_at);
-        if (warp < W && cur.np > 0) ql.template issue<ROWS>(a, cur, g, t);      // ahead of the flood of page loads
+        if (cons < W && cur.np > 0) ql.template issue<ROWS>(a, cur, g, t);      // ahead of the flood of page loads
         if (lane == 0) {
-            begin_of[warp] = cur;
-            first_page[warp] = index;
-            if (warp < W) {
+            if (half == 0) {
+                begin_of[cons] = cur;
+                first_page[cons] = index;
+            }
+            if (cons < W) {
                 now[warp][0] = cur.b; now[warp][1] = cur.u; now[warp][2] = cur.p; now[warp][3] = cur.np; now[warp][4] = seg_at;
             }
         }
         if (tid == 0) { plan[0] = total; plan[1] = ctas; plan[2] = cta0; plan[3] = cta1; }
     }
     __syncthreads();
-    if (warp < W && lane == 0) now[warp][5] = first_page[warp + 1] - first_page[warp];
+    if (cons < W && lane == 0) now[warp][5] = first_page[cons + 1] - first_page[cons];
     __syncwarp();
-    if (warp == W) {
+    if (cons == W) {
         // ---- loads: lane i feeds consumer i, a half page at a time, whenever the consumer has read the one before
         if (lane < W) {
             Cursor ld = begin_of[lane];
@@ -362,7 +381,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
     uint32_t phase = 0;
     bool ok = true;
 #pragma unroll 1
-    while (warp < W && now[warp][5] > 0) {
+    while (cons < W && now[warp][5] > 0) {
         // ---- a segment: query operands
         Cursor cur{now[warp][0], now[warp][1], now[warp][2], now[warp][3]};
         const int kv = kv_of(a, cur.u), len = c.len(cur.b);
@@ -446,13 +465,13 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
             full = min(full, __shfl_xor_sync(0xffffffffu, full, 1));
             full = min(full, __shfl_xor_sync(0xffffffffu, full, 2));
         }
-        float o[D / 16][NT][4], m[NT][2], l[NT][2];
+        float o[CJ][NT][4], m[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             m[nt][0] = m[nt][1] = -INFINITY;
             l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j)
+            for (int j = 0; j < CJ; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[j][nt][e] = 0.f;
         }
@@ -460,61 +479,63 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
 #pragma unroll 1
         for (int p = cur.p; p < end_p; ++p) {
             // ---- S = K q~
-            if (!__all_sync(0xffffffffu, mbar_wait(bars, phase))) { ok = false; break; }
-            const bool there = page_there[warp];
-            float s[4][NT][4];
-            uint32_t qf[NT][NG][2][4];
+            const bool k_in = __all_sync(0xffffffffu, mbar_wait(bars, phase));
+            if (PAIR == 1 && !k_in) { ok = false; break; }
+            const bool there = page_there[cons];
+            float s[TI][NT][4];
+            constexpr int GS = NG < 2 ? NG : 2;                       // groups at a time
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int G0 = 0; G0 < NG; G0 += GS) {
+                uint32_t qf[NT][GS][2][4];
 #pragma unroll
-                for (int G = 0; G < NG; ++G)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const uint4 v = lds128(qbuf + (nt * NG + G) * 1024 + 512 * x);
-                        qf[nt][G][x][0] = v.x; qf[nt][G][x][1] = v.y; qf[nt][G][x][2] = v.z; qf[nt][G][x][3] = v.w;
-                    }
+                    for (int G = 0; G < GS; ++G)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t w[2][NG][2], shw[2][NG];
-                float sc[2][NG];
+                        for (int x = 0; x < 2; ++x) {
+                            const uint4 v = lds128(qbuf + (nt * NG + G0 + G) * 1024 + 512 * x);
+                            qf[nt][G][x][0] = v.x; qf[nt][G][x][1] = v.y; qf[nt][G][x][2] = v.z; qf[nt][G][x][3] = v.w;
+                        }
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int row = 16 * i + 8 * r + g;
-                    const uint32_t wa = kb + P::K_CODES + row * (D / 2) + t * 8 * NG;
-                    if constexpr (NG == 1) {
-                        const uint2 x = lds64(wa);
-                        w[r][0][0] = x.x; w[r][0][1] = x.y;
-                    } else {
+                for (int i = 0; i < TI; ++i) {
+                    uint32_t w[2][GS][2], shw[2][GS];
+                    float sc[2][GS];
 #pragma unroll
-                        for (int G = 0; G < NG; G += 2) {
-                            const uint4 x = lds128(wa + 8 * G);
-                            w[r][G][0] = x.x; w[r][G][1] = x.y; w[r][G + 1][0] = x.z; w[r][G + 1][1] = x.w;
+                    for (int r = 0; r < 2; ++r) {
+                        const int row = 16 * (TI * half + i) + 8 * r + g;
+                        const uint32_t wa = kb + P::K_CODES + row * (D / 2) + t * 8 * NG + 8 * G0;
+                        if constexpr (GS == 1) {
+                            const uint2 x = lds64(wa);
+                            w[r][0][0] = x.x; w[r][0][1] = x.y;
+                        } else {
+                            const uint4 x = lds128(wa);
+                            w[r][0][0] = x.x; w[r][0][1] = x.y; w[r][1][0] = x.z; w[r][1][1] = x.w;
+                        }
+#pragma unroll
+                        for (int G = 0; G < GS; ++G) {
+                            shw[r][G] = lds32(kb + P::K_SHIFTS + 4 * (row * NG + G0 + G));
+                            sc[r][G] = half_scale(lds8(kb + P::K_SCALES + row * NG + G0 + G));
                         }
                     }
 #pragma unroll
-                    for (int G = 0; G < NG; ++G) {
-                        shw[r][G] = lds32(kb + P::K_SHIFTS + 4 * (row * NG + G));
-                        sc[r][G] = half_scale(lds8(kb + P::K_SCALES + row * NG + G));
-                    }
-                }
+                    for (int G = 0; G < GS; ++G) {
+                        uint32_t A[2][2][4];                              // [row half][unit][step]
 #pragma unroll
-                for (int G = 0; G < NG; ++G) {
-                    uint32_t A[2][2][4];                              // [row half][unit][step]
+                        for (int r = 0; r < 2; ++r) {
+                            const uint32_t y = turn(shw[r][G], t);
+                            unpack8(w[r][G][0], y, a.one, A[r][0]);
+                            unpack8(w[r][G][1], y >> 2, a.one, A[r][1]);
+                        }
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const uint32_t y = turn(shw[r][G], t);
-                        unpack8(w[r][G][0], y, a.one, A[r][0]);
-                        unpack8(w[r][G][1], y >> 2, a.one, A[r][1]);
-                    }
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float acc[4];
+                            mma16816_first(acc, A[0][0][0], A[1][0][0], A[0][1][0], A[1][1][0], qf[nt][G][0][0], qf[nt][G][1][0]);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        float acc[4];
-                        mma16816_first(acc, A[0][0][0], A[1][0][0], A[0][1][0], A[1][1][0], qf[nt][G][0][0], qf[nt][G][1][0]);
+                            for (int x = 1; x < 4; ++x)
+                                mma16816(acc, A[0][0][x], A[1][0][x], A[0][1][x], A[1][1][x], qf[nt][G][0][x], qf[nt][G][1][x]);
 #pragma unroll
-                        for (int x = 1; x < 4; ++x)
-                            mma16816(acc, A[0][0][x], A[1][0][x], A[0][1][x], A[1][1][x], qf[nt][G][0][x], qf[nt][G][1][x]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[i][nt][e] = G ? fmaf(acc[e], sc[e >> 1][G], s[i][nt][e]) : acc[e] * sc[e >> 1][G];
+                            for (int e = 0; e < 4; ++e) s[i][nt][e] = G0 + G ? fmaf(acc[e], sc[e >> 1][G], s[i][nt][e]) : acc[e] * sc[e >> 1][G];
+                        }
                     }
                 }
             }
@@ -523,34 +544,45 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
             // ---- softmax of the page's tokens; lane: rows 16 i + g and 16 i + 8 + g, columns 2 t and 2 t + 1
             if (64 * p + 64 > full || !there) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < TI; ++i)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (!there || 64 * p + 16 * i + 8 * (e >> 1) + g >= limit[nt][e & 1]) s[i][nt][e] = -INFINITY;
+                            if (!there || 64 * p + 16 * (TI * half + i) + 8 * (e >> 1) + g >= limit[nt][e & 1]) s[i][nt][e] = -INFINITY;
             }
             bool moved = false;
-            float f[NT][2];
-            uint32_t pw[NT][2][4];
+            float f[NT][2], mx[NT][2];
+            uint32_t pw[NT][2][TI];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    mx[nt][e] = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < TI; ++i) mx[nt][e] = max3(mx[nt][e], s[i][nt][e], s[i][nt][e + 2]);
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) mx[nt][e] = fmaxf(mx[nt][e], __shfl_xor_sync(0xffffffffu, mx[nt][e], x));
+                }
+            if constexpr (PAIR == 2) {
+                if (g == 0) { pair_max[cons][half][2 * t] = mx[0][0]; pair_max[cons][half][2 * t + 1] = mx[0][1]; }
+                if (!pair_sync(cons, k_in)) { ok = false; break; }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) mx[0][e] = fmaxf(mx[0][e], pair_max[cons][half ^ 1][2 * t + e]);
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = -INFINITY;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mx = max3(mx, s[i][nt][e], s[i][nt][e + 2]);
-#pragma unroll
-                    for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
                     // the reference lies 15 below the maximum, so that P <= 2^15 fills the range of FP16
-                    const float mn = fmaxf(m[nt][e], fmaf(mx, f_log2[nt][e], -15.f));
+                    const float mn = fmaxf(m[nt][e], fmaf(mx[nt][e], f_log2[nt][e], -15.f));
                     const float ref = mn == -INFINITY ? 0.f : mn;
                     f[nt][e] = ex2_approx(m[nt][e] - ref);
                     moved |= mn != m[nt][e];
                     m[nt][e] = mn;
                     float sum = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < TI; ++i) {
                         const float p0 = ex2_approx(fmaf(s[i][nt][e], f_log2[nt][e], -ref));
                         const float p1 = ex2_approx(fmaf(s[i][nt][e + 2], f_log2[nt][e], -ref));
                         sum += p0 + p1;
@@ -560,13 +592,14 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
                     if (a.page_ml) {
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-                        if (g == 0 && stat_row[nt][e] >= 0) a.page_ml[(long long)stat_row[nt][e] * c.max_pages + p] = make_float2(mn, sum);
+                        if (PAIR == 2 && g == 0) pair_sum[cons][half][2 * t + e] = sum;
+                        if (PAIR == 1 && g == 0 && stat_row[nt][e] >= 0) a.page_ml[(long long)stat_row[nt][e] * c.max_pages + p] = make_float2(mn, sum);
                     }
                 }
             }
             if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j)
+                for (int j = 0; j < CJ; ++j)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -579,9 +612,20 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sts32(pbuf + 4 * (nt * 8 * C::PV_ROW + (2 * t + e) * C::PV_ROW + 8 * i + g), pw[nt][e][i]);
+                    for (int i = 0; i < TI; ++i) sts32(pbuf + 4 * (nt * 8 * C::PV_ROW + (2 * t + e) * C::PV_ROW + 8 * (TI * half + i) + g), pw[nt][e][i]);
             }
-            __syncwarp();
+            const bool v_in = PAIR == 1 || __all_sync(0xffffffffu, mbar_wait(bars + 8, phase));
+            if constexpr (PAIR == 1) {
+                __syncwarp();
+            } else {
+                if (!pair_sync(cons, v_in)) { ok = false; break; }
+                if (a.page_ml && half == 0 && g == 0)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (stat_row[0][e] >= 0)
+                            a.page_ml[(long long)stat_row[0][e] * c.max_pages + p] =
+                                make_float2(m[0][e], pair_sum[cons][0][2 * t + e] + pair_sum[cons][1][2 * t + e]);
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const uint32_t pa = pbuf + 4 * (nt * 8 * C::PV_ROW + g * C::PV_ROW + 8 * t);
@@ -590,15 +634,15 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
                 pf[nt][4] = hi.x; pf[nt][5] = hi.y; pf[nt][6] = hi.z; pf[nt][7] = hi.w;
             }
             // ---- O += V^T P
-            if (!__all_sync(0xffffffffu, mbar_wait(bars + 8, phase))) { ok = false; break; }
+            if (PAIR == 1 && !__all_sync(0xffffffffu, mbar_wait(bars + 8, phase))) { ok = false; break; }
             if (there) {
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) {
+                for (int j = 0; j < CJ; ++j) {
                     uint32_t A[2][2][4];
                     float sc[2];
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const int ch = 16 * j + 8 * r + g;
+                        const int ch = 16 * (CJ * half + j) + 8 * r + g;
                         const uint2 w = lds64(vb + P::K_CODES + ch * 32 + t * 8);
                         const uint32_t y = turn(lds32(vb + P::K_SHIFTS + 4 * ch), t);
                         sc[r] = half_scale(lds8(vb + P::K_SCALES + ch));
@@ -633,10 +677,16 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
             for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], x);
+        if constexpr (PAIR == 2) {                                   // (and both have read their last page)
+            if (g == 0) { pair_l[cons][half][2 * t] = l[0][0]; pair_l[cons][half][2 * t + 1] = l[0][1]; }
+            pair_sync(cons, true);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) l[0][e] = pair_l[cons][0][2 * t + e] + pair_l[cons][1][2 * t + e];
+        }
         cur = Cursor{now[warp][0], now[warp][1], now[warp][2], now[warp][3]};
         const int seg_at = now[warp][4], remaining = now[warp][5] - (end_p - cur.p);
         const bool begins = cur.p == 0, ends = end_p == cur.np;
-        if (begins && a.seg_ctas && lane == 0)                      // for the page weights: the CTAs that hold the segment
+        if (begins && a.seg_ctas && half == 0 && lane == 0)                      // for the page weights: the CTAs that hold the segment
             a.seg_ctas[(long long)cur.b * units_per_seq(a) + cur.u] = make_int2(blockIdx.x, Shares(plan[0], plan[1]).owner(seg_at + 2 * cur.np - 1));
         if (begins && ends) {
 #pragma unroll
@@ -647,36 +697,36 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
                     if (!row_of<ROWS>(a, cur.u, nt * 8 + 2 * t + e, head, tok)) continue;
                     const float inv = l[nt][e] == 0.f ? 0.f : 1.f / l[nt][e];
 #pragma unroll
-                    for (int j = 0; j < D / 16; ++j) {
-                        store_out(a, cur.b, head, tok, D, 16 * j + g, o[j][nt][e] * inv);
-                        store_out(a, cur.b, head, tok, D, 16 * j + 8 + g, o[j][nt][e + 2] * inv);
+                    for (int j = 0; j < CJ; ++j) {
+                        store_out(a, cur.b, head, tok, D, 16 * (CJ * half + j) + g, o[j][nt][e] * inv);
+                        store_out(a, cur.b, head, tok, D, 16 * (CJ * half + j) + 8 + g, o[j][nt][e + 2] * inv);
                     }
-                    if (g == 0) store_row_stats(a, cur.b, head, tok, m[nt][e], l[nt][e]);
+                    if (half == 0 && g == 0) store_row_stats(a, cur.b, head, tok, m[nt][e], l[nt][e]);
                 }
         } else {
             const int slot = begins ? 1 : 0;
             // the last piece goes where the page was; one that others follow, to global memory
-            float* po = remaining == 0 ? reinterpret_cast<float*>(smem + warp * C::PER_WARP)
-                                       : a.first + ((long long)blockIdx.x * W + warp) * C::PIECE;
+            float* po = remaining == 0 ? reinterpret_cast<float*>(smem + cons * C::PER_WARP)
+                                       : a.first + ((long long)blockIdx.x * W + cons) * C::PIECE;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int r = nt * 8 + 2 * t + e;
 #pragma unroll
-                    for (int j = 0; j < D / 16; ++j) {
-                        po[r * D + 16 * j + g] = o[j][nt][e];
-                        po[r * D + 16 * j + 8 + g] = o[j][nt][e + 2];
+                    for (int j = 0; j < CJ; ++j) {
+                        po[r * D + 16 * (CJ * half + j) + g] = o[j][nt][e];
+                        po[r * D + 16 * (CJ * half + j) + 8 + g] = o[j][nt][e + 2];
                     }
-                    if (g == 0) {
+                    if (half == 0 && g == 0) {
                         po[ROWS * D + 2 * r] = m[nt][e];
                         po[ROWS * D + 2 * r + 1] = l[nt][e];
                     }
                 }
-            if (lane == 0) {
-                piece[2 * warp + slot] = cur;
-                piece_at[2 * warp + slot] = seg_at;
-                piece_of[2 * warp + slot] = po;
+            if (half == 0 && lane == 0) {
+                piece[2 * cons + slot] = cur;
+                piece_at[2 * cons + slot] = seg_at;
+                piece_of[2 * cons + slot] = po;
             }
         }
         // next segment
@@ -728,7 +778,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
         const int kv = kv_of(a, sg.u);                               // (a block of rows that this KV head does not have: none)
         const int rows = max(0, min(ROWS, (a.units.first[kv + 1] - a.units.first[kv]) * a.N - (sg.u - kv * a.blocks) * ROWS));
 #pragma unroll 1
-        for (; turn < rows; turn += W + 1) {
+        for (; turn < rows; turn += C::WARPS) {
             const int r = turn;
             const float* const po = piece_of[mine ? lane : lead];
             const float m = mine ? po[ROWS * D + 2 * r] : -INFINITY, l = mine ? po[ROWS * D + 2 * r + 1] : 0.f;
