@@ -204,10 +204,10 @@ struct TileLayout {
 };
 
 // Rows per KV head from which the tensor-memory kernel is the faster one (us, decode kernel and it; 32 / 8 heads, d = 128, BF16): 8
-// sequences of 4096, 8 rows 22.4 and 38.7, 16 31.7 and 39.5, 32 47.4 and 40.2, 128 138 and 46; 32 of 2048, 16 rows 54 and 66, 32 86
-// and 68; one of 16384, 16 rows 24.5 and 26.4, 32 31.8 and 27.2; FP16, 16 of 1000, 16 rows 25.5 and 23.5; d = 64, FP16, 4 of
-// 1500, 8 rows 10.9 and 13.6, 16 14.4 and 13.6.  d = 256, whose decode kernel takes 8 rows at a time: 8 of 4096, 8 rows 41 and 55, 16
-// 65 and 56.
+// sequences of 4096, 8 rows 20.8 and 38.7, 16 31.0 and 39.4, 32 46.5 and 40.1, 128 133 and 46; 32 of 2048, 16 rows 52 and 66, 32 84
+// and 68; one of 16384, 16 rows 23.8 and 26.2, 32 31.2 and 27.2; FP16, 16 of 1000, 16 rows 24.8 and 23.4; d = 64, FP16, 4 of
+// 1500, 8 rows 10.4 and 13.6, 16 13.0 and 13.6.  d = 256, whose decode kernel takes 8 rows at a time: 8 of 4096, 8 rows 37 and 55, 16
+// 57 and 56.  (One sequence of 300 takes 11 and 10 us at 2 to 8 rows; the host does not know lengths.)
 bool tile_kernel_faster(int d, int rows) { return rows > (d == 256 ? 8 : 16); }
 
 // Workspace of a call; 0 where it is not built.
