@@ -354,7 +354,8 @@ int hifa4_attention_fwd_raw(const hifa4_shape* shape, const void* q, const void*
  * hifa4_cache_append may write the same page or tail.
  *
  * hifa4_strides: distance in elements between consecutive batch rows, heads and tokens of a 16-bit tensor whose channels are
- * contiguous; multiples of 8, the tensor 16-byte aligned.  NULL: contiguous [B][H][tokens][d].
+ * contiguous; multiples of 8, the tensor 16-byte aligned.  NULL: contiguous [B][H][tokens][d].  Factors (s, inv_s) and the
+ * outputs of hifa4_cache_read are 16-byte aligned.
  * ------------------------------------------------------------------------- */
 enum { HIFA4_PAGE_TOKENS = 64 };
 typedef struct {

@@ -38,6 +38,9 @@ int check_tensor(const void* p, const hifa4_strides* st, int H, int n, int d, St
     return HIFA4_OK;
 }
 
+// Factors of Smooth-QK, read four at a time; null: none.
+bool factors_ok(const float* s) { return !((uintptr_t)s & 15); }
+
 CacheView view(const hifa4_cache* c, const hifa4_seqs* s, int* d_status)
 {
     CacheView v;
@@ -126,13 +129,13 @@ void common_args(Args& a, const hifa4_cache* cache, const hifa4_seqs* seqs, cons
 }
 
 int check_call(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
-               const hifa4_strides* q_strides, const void* out, CacheUnits* units, int* rows, Strides* qs)
+               const hifa4_strides* q_strides, const float* s, const void* out, CacheUnits* units, int* rows, Strides* qs)
 {
     int rc = check_cache(cache, false);
     if (rc) return rc;
     if ((rc = check_seqs(seqs, cache->Hkv))) return rc;
     if ((rc = check_query(cache, query, units, rows))) return rc;
-    if (!out || ((uintptr_t)out & 15)) return HIFA4_ERR_INVALID_ARG;
+    if (!out || ((uintptr_t)out & 15) || !factors_ok(s)) return HIFA4_ERR_INVALID_ARG;
     return check_tensor(q, q_strides, query->Hq, query->N, cache->d, qs);
 }
 
@@ -238,7 +241,7 @@ int hifa4_cache_append(const hifa4_cache* cache, const hifa4_seqs* seqs, int n, 
     int rc = check_cache(cache, true);
     if (rc) return rc;
     if ((rc = check_seqs(seqs, cache->Hkv))) return rc;
-    if (n <= 0) return HIFA4_ERR_INVALID_ARG;
+    if (n <= 0 || !factors_ok(inv_s)) return HIFA4_ERR_INVALID_ARG;
     Strides ks, vs;
     if ((rc = check_tensor(k, k_strides, cache->Hkv, n, cache->d, &ks))) return rc;
     if ((rc = check_tensor(v, v_strides, cache->Hkv, n, cache->d, &vs))) return rc;
@@ -253,7 +256,7 @@ int hifa4_cache_read(const hifa4_cache* cache, const hifa4_seqs* seqs, int n, co
     int rc = check_cache(cache, false);
     if (rc) return rc;
     if ((rc = check_seqs(seqs, cache->Hkv))) return rc;
-    if (n <= 0 || !k_out || !v_out) return HIFA4_ERR_INVALID_ARG;
+    if (n <= 0 || !k_out || !v_out || (((uintptr_t)k_out | (uintptr_t)v_out) & 15)) return HIFA4_ERR_INVALID_ARG;
     if (out_dtype < HIFA4_F16 || out_dtype > HIFA4_F32) return HIFA4_ERR_INVALID_ARG;
     if (out_dtype == HIFA4_F16) return HIFA4_ERR_UNSUPPORTED;        // does not hold every HIF4 value
     if ((rc = check_arch())) return rc;
@@ -276,7 +279,9 @@ int hifa4_cache_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const h
     CacheUnits units;
     int rows;
     Strides qs;
-    const int rc = check_call(cache, seqs, query, q, q_strides, out, &units, &rows, &qs);
+    hifa4_strides one_token{};
+    if (q_strides) one_token = hifa4_strides{q_strides->b, q_strides->h, 0};
+    const int rc = check_call(cache, seqs, query, q, q_strides ? &one_token : nullptr, s, out, &units, &rows, &qs);
     if (rc) return rc;
     return run_decode(cache, seqs, query, units, rows, qs, q, s, out, lse, page_weight, page_weight_out, workspace, workspace_bytes,
                       d_status, stream);
@@ -295,7 +300,7 @@ int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, cons
     CacheUnits units;
     int rows;
     Strides qs;
-    int rc = check_call(cache, seqs, query, q, q_strides, out, &units, &rows, &qs);
+    int rc = check_call(cache, seqs, query, q, q_strides, s, out, &units, &rows, &qs);
     if (rc) return rc;
     if (!tile_kernel_faster(cache->d, rows))
         return run_decode(cache, seqs, query, units, rows, qs, q, s, out, nullptr, nullptr, nullptr, workspace, workspace_bytes, d_status, stream);

@@ -109,6 +109,32 @@ def test_attention_refuses_tensors_and_workspaces(hb):
         assert call() in (4, 5)                          # a well-formed call is refused for want of a device, never run on the CPU
 
 
+def test_refuses_what_wide_loads_and_stores_cannot_take(hb):
+    """Factors are read and the cache's values stored 16 bytes at a time."""
+    c, s, q = _cache(hb), _seqs(hb), _query(hb)
+    for off, want in ((0, (4, 5)), (4, (1,)), (8, (1,))):
+        got = [hb.lib().hifa4_cache_read(_p(c), _p(s), 1, None, hb.BF16, 256 + off, 256, None, None),
+               hb.lib().hifa4_cache_read(_p(c), _p(s), 1, None, hb.F32, 256, 256 + off, None, None),
+               hb.lib().hifa4_cache_append(_p(c), _p(s), 1, None, 256, None, 256, None, 256 + off, None, None),
+               hb.lib().hifa4_cache_decode(_p(c), _p(s), _p(q), 256, None, 256 + off, 256, None, None, None, 256, 1 << 40, None, None),
+               hb.lib().hifa4_cache_attention(_p(c), _p(s), _p(_query(hb, N=40)), 256, None, 256 + off, 256, 256, 1 << 40, None, None)] \
+            if off or not _has_gpu() else []
+        assert all(g in want for g in got), (off, got)
+
+
+def test_decode_does_not_look_at_the_token_stride(hb):
+    """q of one token: what the third stride holds does not matter (hifa4.h: unused)."""
+    if not _has_gpu():
+        st = hb._Strides(4096, 128, 3)
+        assert hb.lib().hifa4_cache_decode(_p(_cache(hb)), _p(_seqs(hb)), _p(_query(hb)), 256, _p(st), None, 256, None, None, None, 256,
+                                           1 << 40, None, None) in (4, 5)
+
+
+def _has_gpu():
+    import torch
+    return torch.cuda.is_available()                     # (made-up addresses are for hosts without one)
+
+
 def test_evict_refuses(hb):
     f = hb.lib().hifa4_cache_evict
 
