@@ -132,7 +132,6 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
     const uint32_t bars = smem + C::MISC_OFF;
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (tid == 0) {
         for (int i = 0; i < 3; ++i) {
             mbar_init(bar(RF + i), 1); mbar_init(bar(RE + i), 4);
@@ -144,10 +143,13 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
         fence_barrier_init();
         abort_flag = 0;
     }
+    // Tensor memory is taken when the kernel before is over, and the next one may start when every CTA has its own: of two kernels
+    // on an SM none waits for columns that the other holds while it waits for the whole grid.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (warp == C::W_MMA) { tmem_alloc(smem_u32(&tmem_slot), 512); tmem_relinquish(); }
     tc_fence_before();
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
 
