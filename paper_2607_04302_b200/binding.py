@@ -561,6 +561,11 @@ def _seqs(block_table, kv_lens, dev, tail_slots=None) -> _Seqs:
     return _Seqs(B, max_pages, block_table.data_ptr(), kv_lens.data_ptr(), None if tail_slots is None else tail_slots.data_ptr())
 
 
+def _status(t, dev):
+    assert t is None or (t.dtype is _I32 and t.get_device() == dev)
+    return _ptr(t)
+
+
 def _strides(t, dev):
     """Reference to the strides of [B,H,n,d] or [B,H,d] (channels contiguous), None where all is contiguous."""
     assert t.get_device() == dev
@@ -581,7 +586,7 @@ def cache_append(cache: PagedCache, k, v, block_table, kv_lens, n_new=None, inv_
     assert cache.v_tail is not None and cache.v_tail.dtype is dt
     assert (n_new is None or _ok(n_new, _I32, shape[:1], dev)) and (inv_s is None or _ok(inv_s, _FP32, (Hkv, d), dev))
     rc = lib().hifa4_cache_append(C.byref(st), C.byref(sq), n, _ptr(n_new), k.data_ptr(), _strides(k, dev), v.data_ptr(),
-                                  _strides(v, dev), _ptr(inv_s), _ptr(d_status), _raw_stream(dev))
+                                  _strides(v, dev), _ptr(inv_s), _status(d_status, dev), _raw_stream(dev))
     if rc:
         _check(rc, "hifa4_cache_append")
 
@@ -595,7 +600,7 @@ def cache_read(cache: PagedCache, block_table, kv_lens, n, start=None, out_dtype
     k, v = out if out is not None else [cache.pages.new_empty(shape, dtype=_TORCH_DT[out_dtype]) for _ in range(2)]
     dt = k.dtype
     assert _ok(k, dt, shape, dev) and _ok(v, dt, shape, dev) and (start is None or _ok(start, _I32, shape[:1], dev))
-    rc = lib().hifa4_cache_read(C.byref(st), C.byref(sq), n, _ptr(start), _DT[dt], k.data_ptr(), v.data_ptr(), _ptr(d_status),
+    rc = lib().hifa4_cache_read(C.byref(st), C.byref(sq), n, _ptr(start), _DT[dt], k.data_ptr(), v.data_ptr(), _status(d_status, dev),
                                 _raw_stream(dev))
     if rc:
         _check(rc, "hifa4_cache_read")
@@ -646,7 +651,7 @@ def cache_decode(q, cache: PagedCache, block_table, kv_lens, s=None, out=None, l
     keep, mp = _map_arr(q_to_kv)
     rc = lib().hifa4_cache_decode(C.byref(st), C.byref(sq), C.byref(_CacheQuery(Hq, mp, 1, 0, _DT[out.dtype], softmax_scale)),
                                   q.data_ptr(), _strides(q, dev), _ptr(s), out.data_ptr(), _ptr(lse), _ptr(page_weight),
-                                  _ptr(page_weight_out), workspace.data_ptr(), workspace.nbytes, _ptr(d_status), _raw_stream(dev))
+                                  _ptr(page_weight_out), workspace.data_ptr(), workspace.nbytes, _status(d_status, dev), _raw_stream(dev))
     if rc:
         _check(rc, "hifa4_cache_decode")
     return out
@@ -680,7 +685,7 @@ def cache_attention(q, cache: PagedCache, block_table, kv_lens, causal, s=None, 
     keep, mp = _map_arr(q_to_kv)
     rc = lib().hifa4_cache_attention(C.byref(st), C.byref(sq), C.byref(_CacheQuery(Hq, mp, N, causal, _DT[out.dtype], softmax_scale)),
                                      q.data_ptr(), _strides(q, dev), _ptr(s), out.data_ptr(), workspace.data_ptr(), workspace.nbytes,
-                                     _ptr(d_status), _raw_stream(dev))
+                                     _status(d_status, dev), _raw_stream(dev))
     if rc:
         _check(rc, "hifa4_cache_attention")
     return out
@@ -716,7 +721,7 @@ def cache_evict(block_table, kv_lens, page_weight, keep_pages, keep_first=1, kee
     assert _ok(out.page_weight, _FP32, shape, dev) and _ok(out.freed, _I32, shape, dev) and _ok(out.n_freed, _I32, lens, dev)
     rc = lib().hifa4_cache_evict(C.byref(sq), page_weight.data_ptr(), keep_pages, keep_first, keep_last, out.block_table.data_ptr(),
                                  out.kv_lens.data_ptr(), out.page_weight.data_ptr(), out.freed.data_ptr(), out.n_freed.data_ptr(),
-                                 _ptr(d_status), _raw_stream(dev))
+                                 _status(d_status, dev), _raw_stream(dev))
     if rc:
         _check(rc, "hifa4_cache_evict")
     return out

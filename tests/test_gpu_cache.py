@@ -519,6 +519,49 @@ def test_binding_refuses_tensors():
         hb().cache_evict(table, ints([100]), torch.zeros(table.shape, device=DEV), 1, 1, 1)
 
 
+def test_binding_refuses_host_status_words_and_unaligned_factors():
+    cache, table, k, v, s, inv_s = make_cache([100], 2, 64, "fp16")
+    q, kv, status = torch.randn((1, 4, 64), device=DEV).half(), ints([100]), torch.zeros(1, dtype=torch.int32)
+    w = torch.zeros(table.shape, device=DEV)
+    for call in (lambda: hb().cache_decode(q, cache, table, kv, d_status=status), lambda: hb().cache_read(cache, table, kv, 4, d_status=status),
+                 lambda: hb().cache_attention(q[:, :, None], cache, table, kv, False, d_status=status),
+                 lambda: hb().cache_append(cache, k.to(DEV), v.to(DEV), table, kv, d_status=status),
+                 lambda: hb().cache_evict(table, kv, w, 1, 0, 1, d_status=status)):
+        with pytest.raises(AssertionError):
+            call()
+    off = torch.ones(2 * 64 + 1, device=DEV)[1:].view(2, 64)
+    out = [torch.empty(2 * 4 * 64 + 1, device=DEV)[1:].view(1, 2, 4, 64) for _ in range(2)]
+    for call in (lambda: hb().cache_decode(q, cache, table, kv, s=off), lambda: hb().cache_append(cache, k.to(DEV), v.to(DEV), table, kv, inv_s=off),
+                 lambda: hb().cache_attention(q[:, :, None], cache, table, kv, False, s=off), lambda: hb().cache_read(cache, table, kv, 4, out=out)):
+        with pytest.raises(hb().Hifa4Error):
+            call()
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "fp16"), (128, "bf16"), (256, "bf16")])
+def test_between_other_kernels(d, dtype):
+    """Calls that follow one another on a stream, each of which may start before the one before has ended: prefill attention, decode,
+    attention of many tokens, appends, over and over, give what each gives alone."""
+    lens = [1000, 130]
+    cache, table, k, v, s, inv_s = make_cache(lens, 2, d, dtype)
+    kv, kd, vd = ints(lens), k.to(DEV), v.to(DEV)
+    gen = torch.Generator().manual_seed(8)
+    qn = torch.randn((2, 4, 192, d), generator=gen).to(DT[dtype]).to(DEV)
+    kp, vp = (torch.randn((2, 2, 192, d), generator=gen).to(DT[dtype]).to(DEV) for _ in range(2))
+    q1 = qn[:, :, 0].contiguous()
+    calls = [lambda: hb().cache_attention(qn, cache, table, kv, True, s=s), lambda: hb().attention_fwd_raw(qn, kp, vp, s, inv_s, True),
+             lambda: hb().cache_attention(qn, cache, table, kv, False, s=s), lambda: hb().cache_decode(q1, cache, table, kv, s=s)]
+    alone = []
+    for call in calls:
+        alone.append(call())
+        torch.cuda.synchronize()
+    for _ in range(10):
+        for i in (0, 0, 1, 0, 2, 3, 1, 1, 3, 2):
+            got = calls[i]()
+            hb().cache_append(cache, kd, vd, table, kv, n_new=kv, inv_s=inv_s)           # (the same values again)
+            again = calls[i]()
+            assert torch.equal(got, alone[i]) and torch.equal(again, alone[i])
+
+
 @pytest.mark.parametrize("counts", [(17, 0, 3), (1, 9, 0), (0, 0, 5)])
 @pytest.mark.parametrize("N", [1, 2, 24])
 def test_uneven_head_maps(counts, N):
