@@ -210,20 +210,19 @@ __device__ __forceinline__ void store8(float* p, const uint32_t (&x)[4])
     reinterpret_cast<uint4*>(p)[1] = make_uint4(x[2] << 16, x[2] & 0xFFFF0000u, x[3] << 16, x[3] & 0xFFFF0000u);
 }
 
-// One CTA per (sequence, KV head, page): the page's codes to shared memory, half of the threads on K, half on V.  K: a thread
-// per unit of a row.  V: a thread per word of eight channels, whose 64 values are turned in registers, so that it stores 16
-// bytes (FP32: 32) of eight rows.
+// Two CTAs per (sequence, KV head, page), one for K and one for V; both straight from global memory (32K tokens of 8 heads, d = 128: 27
+// us, the copy rate; by way of shared memory in one CTA 38).  K: a thread per unit of a row.  V: a thread per word of eight
+// channels, whose 64 values are turned in registers, so that it stores 16 bytes (FP32: 32) of eight rows; a warp has four words of
+// 64 channels and stores whole 128-byte lines (eight words of 32 channels: 32 us).
 template <typename O, int D>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(128, 10)
 cache_read_kernel(const CacheView c, int n, const int* __restrict__ start, O* __restrict__ k_out, O* __restrict__ v_out)
 {
     using P = Page<D>;
-    constexpr int NG = P::NG;
-    constexpr int V_AT = P::HALF, V_SHIFTS = V_AT + 36 * D;      // V codes with 32 bytes of padding after every eight channels
-    __shared__ __align__(16) uint8_t sm[V_AT + 41 * D];
+    constexpr int NG = P::NG, AHEAD = 4;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int b = blockIdx.y / c.Hkv, h = blockIdx.y % c.Hkv, tid = threadIdx.x;
+    const int b = blockIdx.y / c.Hkv, h = blockIdx.y % c.Hkv, tid = threadIdx.x + 128 * blockIdx.z;   // from 128: V
     const int len = c.len(b), begin = start ? __ldg(start + b) : 0;
     if (len < 0 || begin < 0) {
         if (blockIdx.x == 0 && tid == 0) c.invalid();
@@ -237,39 +236,52 @@ cache_read_kernel(const CacheView c, int n, const int* __restrict__ start, O* __
         if (tid == 0) c.invalid();
         return;
     }
-    const uint4* src = reinterpret_cast<const uint4*>(c.pages + ((long long)page * c.Hkv + h) * P::BYTES);
-    for (int i = tid; i < P::BYTES / 16; i += 256) {
-        const int v16 = i - P::HALF / 16;                        // 16-byte piece of V's half
-        const int dst = v16 < 0 ? i : P::HALF / 16 + (v16 < 2 * D ? v16 + v16 / 16 * 2 : v16 + D / 4);
-        reinterpret_cast<uint4*>(sm)[dst] = __ldg(src + i);
-    }
-    __syncthreads();
+    const uint8_t* pg = c.pages + ((long long)page * c.Hkv + h) * P::BYTES;
     const int lo = max(begin - 64 * p, 0), hi = min(end - 64 * p, 64);
     const long long row0 = ((long long)b * c.Hkv + h) * n + 64ll * p - begin;
     if (tid < 128) {
-        for (int t = tid; t < 64 * D / 8; t += 128) {
-            const int r = t / (D / 8), u = t % (D / 8), G = u / 8, uu = u % 8;
-            if (r < lo || r >= hi) continue;
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(sm + P::K_CODES + r * (D / 2) + (uu / 2) * 8 * NG + 8 * G + uu % 2 * 4);
-            const uint32_t sh = *reinterpret_cast<const uint32_t*>(sm + P::K_SHIFTS + 4 * (r * NG + G));
-            uint32_t x[4];
-            hif4_word_values(w, shifts_of_unit(sh, uu), scale_pair(sm[P::K_SCALES + r * NG + G]), x);
-            const uint32_t y[4] = {__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410), __byte_perm(x[0], x[1], 0x7632),
-                                   __byte_perm(x[2], x[3], 0x7632)};
-            store8(k_out + (row0 + r) * D + 8 * u, y);
+        const int u = tid % (D / 8), G = u / 8, uu = u % 8;
+        constexpr int ROWS = 128 / (D / 8);                      // rows at a time
+#pragma unroll 1
+        for (int r0 = tid / (D / 8); r0 < 64; r0 += ROWS * AHEAD) {
+            uint32_t w[AHEAD], sh[AHEAD], sc[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int r = r0 + i * ROWS;
+                if (r < lo || r >= hi) continue;
+                w[i] = __ldg(reinterpret_cast<const uint32_t*>(pg + P::K_CODES + r * (D / 2) + (uu / 2) * 8 * NG + 8 * G + uu % 2 * 4));
+                sh[i] = __ldg(reinterpret_cast<const uint32_t*>(pg + P::K_SHIFTS + 4 * (r * NG + G)));
+                sc[i] = __ldg(pg + P::K_SCALES + r * NG + G);
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int r = r0 + i * ROWS;
+                if (r < lo || r >= hi) continue;
+                uint32_t x[4];
+                hif4_word_values(w[i], shifts_of_unit(sh[i], uu), scale_pair(sc[i]), x);
+                const uint32_t y[4] = {__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410), __byte_perm(x[0], x[1], 0x7632),
+                                       __byte_perm(x[2], x[3], 0x7632)};
+                store8(k_out + (row0 + r) * D + 8 * u, y);
+            }
         }
         return;
     }
+    const uint8_t* vp = pg + P::HALF;
+#pragma unroll 1
     for (int t = tid - 128; t < D; t += 128) {
-        const int w = t % 8, o = t / 8;
-        uint32_t x[8][4];                                        // channel 8 o + i: pairs of tokens 16 (w / 2) + 4 (w % 2) + e, + 8
+        const int o = t / 4 % (D / 8), w = t % 4 + t / 4 / (D / 8) * 4;
+        uint32_t code[8], sh[8], x[8][4];                        // channel 8 o + i: pairs of tokens 16 (w / 2) + 4 (w % 2) + e, + 8
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int ch = 8 * o + i;
-            const uint32_t code = *reinterpret_cast<const uint32_t*>(sm + V_AT + ch * 32 + o * 32 + w * 4);
-            const uint32_t sh = *reinterpret_cast<const uint32_t*>(sm + V_SHIFTS + 4 * ch);
-            hif4_word_values(code, shifts_of_unit(sh, w), scale_pair(sm[V_SHIFTS + 4 * D + ch]), x[i]);
+        for (int i = 0; i < 8; ++i) code[i] = __ldg(reinterpret_cast<const uint32_t*>(vp + P::K_CODES + (8 * o + i) * 32 + w * 4));
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const uint4 y = __ldg(reinterpret_cast<const uint4*>(vp + P::K_SHIFTS + 32 * o) + i / 4);
+            sh[i] = y.x; sh[i + 1] = y.y; sh[i + 2] = y.z; sh[i + 3] = y.w;
         }
+        const uint2 sc = __ldg(reinterpret_cast<const uint2*>(vp + P::K_SCALES + 8 * o));
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            hif4_word_values(code[i], shifts_of_unit(sh[i], w), scale_pair((i < 4 ? sc.x : sc.y) >> 8 * (i % 4) & 255), x[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int r = 16 * (w / 2) + 4 * (w % 2) + e % 4 + e / 4 * 8;
@@ -304,7 +316,7 @@ cudaError_t launch_cache_append(int dtype, int d, const CacheView& c, int n, con
 template <typename O, int D>
 static cudaError_t read_d(const CacheView& c, int n, const int* start, void* k, void* v, cudaStream_t st)
 {
-    return launch_dependent(cache_read_kernel<O, D>, dim3((unsigned)((n + 126ll) / 64), (unsigned)(c.B * c.Hkv)), 256, 0, st, c, n, start, (O*)k, (O*)v);
+    return launch_dependent(cache_read_kernel<O, D>, dim3((unsigned)((n + 126ll) / 64), (unsigned)(c.B * c.Hkv), 2), 128, 0, st, c, n, start, (O*)k, (O*)v);
 }
 
 cudaError_t launch_cache_read(int d, const CacheView& c, int n, const int* start, int out_dtype, void* k, void* v, cudaStream_t st)
