@@ -3,14 +3,32 @@
 
 namespace hifa4 {
 
-// Nibbles 8 + m of four biased quotients (hif4_unit: the low byte of bits(y) is the signed code m): elements 0, 1 in byte 0,
-// elements 2, 3 in byte 2.
-__device__ __forceinline__ uint32_t nibbles4(const float* y)
+// Nibbles 8 + m of a subgroup's four codes in the low 16 bits, element i in nibble i (above them: anything).  k: the shift.  As
+// hif4_unit_values, with 8 more in the low bits of the magic constant: the low bits of y are 8 + m, and no carry leaves a nibble when
+// y's multiples by powers of 16 are added up (three instructions for four codes; gathered as bytes and then as nibbles it takes six,
+// and 32K tokens 51 us instead of 48).
+__device__ __forceinline__ uint32_t subgroup_nibbles(const float* x, int k, const Hif4Group& g)
 {
-    const uint32_t b01 = __byte_perm(__float_as_uint(y[0]), __float_as_uint(y[1]), 0x0040);
-    const uint32_t b23 = __byte_perm(__float_as_uint(y[2]), __float_as_uint(y[3]), 0x0040);
-    const uint32_t n = (__byte_perm(b01, b23, 0x5410) & 0x0F0F0F0Fu) ^ 0x08080808u;       // m + 8 modulo 16
-    return n | (n >> 4);
+    const float magic = __uint_as_float(0x4B400008u + ((uint32_t)k << 23));
+    const uint64_t mm = pack2(magic, magic);
+    float y0, y1, y2, y3;
+    unpack2(add2(mul2_rz(pack2(x[0], x[1]), g.inv44), mm), y0, y1);
+    unpack2(add2(mul2_rz(pack2(x[2], x[3]), g.inv44), mm), y2, y3);
+    return __float_as_uint(y3) * 4096 + (__float_as_uint(y2) * 256 + (__float_as_uint(y1) * 16 + __float_as_uint(y0)));
+}
+
+// The larger magnitudes of packed pairs, of either sign.
+template <typename T, bool NAN_WINS> __device__ __forceinline__ uint32_t max_mag(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    if constexpr (__is_same(T, __half)) {
+        if (NAN_WINS) asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else asm("max.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    } else {
+        if (NAN_WINS) asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    }
+    return r;
 }
 
 // Largest magnitude of a group, of which each of four lanes has 16 values (packed pairs).  NAN_WINS: a NaN if there is one, else
@@ -20,8 +38,8 @@ template <typename T, bool NAN_WINS> __device__ __forceinline__ float group_max(
     auto max2 = [](uint32_t a, uint32_t b) { return NAN_WINS ? max16_nan<T>(a, b) : max16<T>(a, b); };
     uint32_t m[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m[i] = max2(abs16<T>(x[i]), abs16<T>(x[i + 4]));
-    m[0] = max2(max2(m[0], m[1]), max2(m[2], m[3]));
+    for (int i = 0; i < 4; ++i) m[i] = max_mag<T, NAN_WINS>(x[i], x[i + 4]);
+    m[0] = abs16<T>(max_mag<T, NAN_WINS>(max_mag<T, NAN_WINS>(m[0], m[1]), max_mag<T, NAN_WINS>(m[2], m[3])));
     m[0] = max2(m[0], __shfl_xor_sync(0xffffffffu, m[0], 1));
     m[0] = max2(m[0], __shfl_xor_sync(0xffffffffu, m[0], 2));
     m[0] = max2(m[0], __byte_perm(m[0], m[0], 0x1032));
@@ -30,14 +48,14 @@ template <typename T, bool NAN_WINS> __device__ __forceinline__ float group_max(
     return a;
 }
 
-// A lane's 16 consecutive values (two units) of a group: nibbles of the four subgroups (nibbles4) and their shifts.
+// A lane's 16 consecutive values (two units) of a group: nibbles of the four subgroups (subgroup_nibbles) and their shifts.
 // GENERAL: what lies above the E6M2 range saturates, a NaN becomes zero; otherwise there are none.
 template <typename T, bool GENERAL>
 __device__ __forceinline__ void quantize16(const uint32_t (&xw)[8], const Hif4Group& g, uint32_t (&nib)[4], int (&k)[4])
 {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        float x[8], y[8];
+        float x[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) Pair16<T>::unpack(xw[4 * u + i], x[2 * i], x[2 * i + 1]);
         if (GENERAL) {
@@ -46,11 +64,12 @@ __device__ __forceinline__ void quantize16(const uint32_t (&xw)[8], const Hif4Gr
         }
         const float a0 = fmaxf(max3(fabsf(x[0]), fabsf(x[1]), fabsf(x[2])), fabsf(x[3]));
         const float a1 = fmaxf(max3(fabsf(x[4]), fabsf(x[5]), fabsf(x[6])), fabsf(x[7]));
-        uint32_t w[4];
-        int a;
-        hif4_unit(x, a0, a1, g, w, y, a, k[2 * u], k[2 * u + 1]);
-        nib[2 * u] = nibbles4(y);
-        nib[2 * u + 1] = nibbles4(y + 4);
+        const int n0 = max((int)__float_as_uint(a0) + g.tadd, 0) >> 23, n1 = max((int)__float_as_uint(a1) + g.tadd, 0) >> 23;
+        const int a = (n0 + n1 + 2) >> 2;                                    // (see hif4_unit)
+        k[2 * u] = max(n0, a);
+        k[2 * u + 1] = max(n1, a);
+        nib[2 * u] = subgroup_nibbles(x, k[2 * u], g);
+        nib[2 * u + 1] = subgroup_nibbles(x + 4, k[2 * u + 1], g);
     }
 }
 // The same from the values alone; *code: the group's scale.  Whole warp: the general form runs where a group of the warp needs it.
@@ -159,7 +178,7 @@ cache_append_kernel(const CacheView c, int n, const int* __restrict__ n_new, con
         s |= __shfl_xor_sync(0xffffffffu, s, 2);
         if (!in) continue;
         *reinterpret_cast<uint2*>(pg + P::K_CODES + r * (D / 2) + j * 8 * NG + 8 * G) =
-            make_uint2(__byte_perm(nib[0], nib[1], 0x6420), __byte_perm(nib[2], nib[3], 0x6420));
+            make_uint2(__byte_perm(nib[0], nib[1], 0x5410), __byte_perm(nib[2], nib[3], 0x5410));
         if (j == 0) {
             *reinterpret_cast<uint32_t*>(pg + P::K_SHIFTS + 4 * (r * NG + G)) = s;
             pg[P::K_SCALES + r * NG + G] = (uint8_t)code;
@@ -193,7 +212,7 @@ cache_append_kernel(const CacheView c, int n, const int* __restrict__ n_new, con
             s |= __shfl_xor_sync(0xffffffffu, s, 2);
             const int ch = 2 * cp + x;
             *reinterpret_cast<uint2*>(vp + P::K_CODES + ch * 32 + j * 8) =
-                make_uint2(__byte_perm(nib[0], nib[2], 0x6420), __byte_perm(nib[1], nib[3], 0x6420));
+                make_uint2(__byte_perm(nib[0], nib[2], 0x5410), __byte_perm(nib[1], nib[3], 0x5410));
             if (j == 0) {
                 *reinterpret_cast<uint32_t*>(vp + P::K_SHIFTS + 4 * ch) = s;
                 vp[P::K_SCALES + ch] = (uint8_t)code;
