@@ -221,6 +221,38 @@ def test_decode_long(lens, B):
     check_attention(out[:, :, None], r, 128)
 
 
+@pytest.mark.parametrize("Hq,Hkv,d,dtype", [(8, 1, 256, "bf16"), (16, 2, 256, "fp16"), (14, 2, 64, "fp16"), (24, 2, 64, "bf16"), (30, 2, 128, "fp16")])
+def test_decode_long_of_every_width(Hq, Hkv, d, dtype):
+    """Segments within a consumer, across consumers and across CTAs, of each head dimension and block of rows, with page weights; then
+    with a page that is not there."""
+    lens = [9000, 130, 3000, 64]
+    cache, table, k, v, s, inv_s = make_cache(lens, Hkv, d, dtype, seed=d)
+    q = (torch.randn((4, Hq, d), generator=torch.Generator().manual_seed(d)) * 2).to(DT[dtype])
+    w = torch.full(table.shape, 7.0, device=DEV)
+
+    def check(out, table, lens, rows, cols):
+        r = ref.attend(q[rows][:, :, None], cache.pages.cpu(), table.cpu(), lens, s.cpu())
+        check_attention(out[rows][:, :, None], r, d)
+        ds = ref.score_error(r.E[..., 0], d)
+        eps = 2 * (torch.expm1(ds).amax(1, keepdim=True) + 2.0 ** -20) + 2.0 ** -20          # as in test_decode_matches_fp64
+        got = w[rows][:, cols].double().cpu()
+        for b, n in enumerate(lens):
+            m = (n + 63) // 64
+            assert ((got[b, :m] - r.weight[b, :m]).abs() <= eps[b] * r.weight[b, :m] + 2.0 ** -23).all()
+
+    out = hb().cache_decode(q.to(DEV), cache, table, ints(lens), s=s, page_weight_out=w)
+    check(out, table, lens, [0, 1, 2, 3], list(range(table.shape[1])))
+    assert (w[1, 3:] == 7).all() and (w[3, 1:] == 7).all()
+    again = hb().cache_decode(q.to(DEV), cache, table, ints(lens), s=s)
+    assert torch.equal(out, again)
+    bad, status = table.clone(), torch.zeros(1, dtype=torch.int32, device=DEV)
+    bad[0, 70] = -1
+    out = hb().cache_decode(q.to(DEV), cache, bad, ints(lens), s=s, page_weight_out=w, d_status=status)
+    cols = [i for i in range(table.shape[1]) if i != 70]
+    check(out, table[:1, cols], [9000 - 64], [0], cols)
+    assert status.item() == 1 and w[0, 70] == 0 and torch.equal(out[1:], again[1:])
+
+
 def test_bad_lengths_and_pages_are_left_out():
     """Found on the device: the sequence (page) is left out, the status word says so, the others are as usual."""
     lens = [200, 130, 64]
