@@ -346,6 +346,23 @@ def test_evict_matches_sorting(B, P, keep, first, last):
         assert np.array_equal(r.freed.cpu().numpy(), want["freed"])
 
 
+def test_evict_whole_classes_of_weights():
+    """The border between what stays and what goes falls between classes of equal weights, inside one, and among NaN; weights that
+    differ in their first, in their last and in no digit."""
+    P = 200
+    low = np.arange(P, dtype=np.uint32) + 0x3F800000                       # differ in their last bits
+    sets = [np.repeat(np.float32([1, 2, 3, 4]), 50), low.view(np.float32), (low * 256).view(np.float32), np.zeros(P, np.float32),
+            np.where(np.arange(P) % 2, np.nan, 1.0).astype(np.float32), np.full(P, np.nan, np.float32), np.repeat(np.float32([-1, -0.0, 0.0, 1]), 50)]
+    weight = np.stack(sets).astype(np.float32)
+    B = len(sets)
+    table, lens = np.tile(np.arange(P, dtype=np.int32), (B, 1)), np.full(B, 64 * P, np.int32)
+    t, l, w = torch.from_numpy(table).to(DEV), torch.from_numpy(lens).to(DEV), torch.from_numpy(weight).to(DEV)
+    for keep in (2, 3, 51, 52, 53, 101, 102, 103, 150, 151, 152, 199, 200):
+        r, want = hb().cache_evict(t, l, w, keep, 1, 1), ref.evict(table, lens, weight, keep, 1, 1)
+        assert np.array_equal(r.block_table.cpu().numpy(), want["table"]) and r.kv_lens.tolist() == want["lens"]
+        assert np.array_equal(r.freed.cpu().numpy(), want["freed"]) and r.n_freed.tolist() == want["n"], keep
+
+
 def test_serving_run():
     """Prompt, twenty steps with page weights, an eviction, more steps over the shorter tables, a second chunk: each against FP64."""
     Hq, Hkv, d = 8, 2, 128
