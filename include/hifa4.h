@@ -168,8 +168,8 @@ const char* hifa4_status_string(int status);
 int hifa4_selftest_wait_timeout(const hifa4_shape* shape, const hifa4_qkv* qkv, const hifa4_attn_params* prm,
                                 void* out, int* d_status, void* stream);
 
-/* Calls made so far in this process: out[0] calibrate, out[1] quantize,
- * out[2] attention, out[3] kernels launched (all entry points). */
+/* Calls made so far in this process: out[0] calibrate, out[1] quantize (hifa4_cache_append too),
+ * out[2] attention (hifa4_cache_decode and hifa4_cache_attention too), out[3] kernels launched (all entry points). */
 void hifa4_get_counters(unsigned long long out[4]);
 
 /* Offline Smooth-QK calibration (Eq. "sqk"; "Calibration-Static Deployment").
