@@ -468,9 +468,14 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
                     }
                 }
             }
-            // the last commits have arrived before this shared memory goes to another CTA
-            if (good) good = tile_wait(bar(KE + (n - 1) % C::KS), (uint32_t)((n - 1) / C::KS) & 1u, &abort_flag) &&
-                             tile_wait(bar(VE + (n - 1) % C::KS), (uint32_t)((n - 1) / C::KS) & 1u, &abort_flag);
+            // Every commit has arrived before this shared memory goes to another CTA, and this tile's O is complete.  The stages of the last
+            // pages are not enough for that: with both tiles on the same rows the last page is one tile's and the other has only
+            // arrived for it, while its own last product may still run.
+            for (int i = max(n - C::KS, 0); i < n && good; ++i)
+                good = tile_wait(bar(KE + i % C::KS), (uint32_t)(i / C::KS) & 1u, &abort_flag) &&
+                       tile_wait(bar(VE + i % C::KS), (uint32_t)(i / C::KS) & 1u, &abort_flag);
+            const int own = alt ? (n + 1 - h) >> 1 : h < tiles ? n : 0;      // pages of this tile
+            if (good && own > 0) good = tile_wait(bar(OD + h), (uint32_t)(own - 1) & 1u, &abort_flag);
             if (!good) { fail(); ok = false; }
         }
         __syncwarp();
@@ -497,7 +502,7 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
     }
     if (!ok) let_copies_land();
     tc_fence_before();
-    __syncthreads();                                                 // every product is complete (the issuers waited for their last ones)
+    __syncthreads();                                                 // every product is complete (each issuer waited for its tile's last one)
     tc_fence_after();
     const bool good = abort_flag == 0;
     const uint32_t t_o = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (h_sm & 1) * D;
