@@ -378,8 +378,15 @@ size_t hifa4_cache_page_bytes(int d);
 
 /* Smooth-QK and HIF4 quantization of new tokens into the cache: k, v [B,Hkv,n,d] of cache->in_dtype; sequence b takes its
  * first n_new[b] tokens (device array; NULL: n of them; 0 allowed) at positions kv_lens[b] - n_new[b] and on.  inv_s: [Hkv,d]
- * factors of K as in hifa4_quantize_qkv, or NULL.  The incomplete page's older values come from v_tail, so a sequence may be
- * cut back (kv_lens lowered) inside its last page only, before the next append; nothing else of a page may be appended again. */
+ * factors of K as in hifa4_quantize_qkv, or NULL.
+ * The older values of a page that is continued come from v_tail.  An append leaves there what the last page may be continued from: the
+ * rows of an incomplete page, and of a page that it completes but did not begin all but the last.  So before the next append a
+ * sequence may be cut back (kv_lens lowered: drafted tokens that were not accepted)
+ *   - to any multiple of 64: the tokens behind it are appended anew;
+ *   - inside its last page, unless that is full and one append filled it from its first position on.
+ * Further back, inside another page, it may not: V's groups would be formed again from rows that v_tail does not hold.  A draft that
+ * crosses into the next page is settled by cutting the sequence back to the first position of the page that it left and appending
+ * that page's accepted tokens again, whose K and V the caller has to have. */
 int hifa4_cache_append(const hifa4_cache* cache, const hifa4_seqs* seqs, int n, const int* n_new, const void* k,
                        const hifa4_strides* k_strides, const void* v, const hifa4_strides* v_strides, const float* inv_s,
                        int* d_status, void* stream);
@@ -414,9 +421,9 @@ int hifa4_cache_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const h
                        float* page_weight_out, void* workspace, size_t workspace_bytes, int* d_status, void* stream);
 
 /* The same for N >= 1 query tokens per sequence: q [B,Hq,N,d], out [B,Hq,N,d].  Cross attention to an encoder's states of other
- * lengths (causal 0), the next chunk of a prompt or several drafted tokens (causal 1, after their append).  More than 16 query rows
- * (heads times tokens; d = 256: 8) per KV head take a kernel on tcgen05 in which P is rounded to BF16, for FP16 activations to two
- * terms of BF16 (16 bits).  The workspace may be used by the next call on the same stream. */
+ * lengths (causal 0), the next chunk of a prompt or several drafted tokens (causal 1, after their append; hifa4_cache_append says how far
+ * they can be taken back).  More than 16 query rows (heads times tokens; d = 256: 8) per KV head take a kernel on tcgen05 in which P is
+ * rounded to BF16, for FP16 activations to two terms of BF16 (16 bits).  The workspace may be used by the next call on the same stream. */
 size_t hifa4_cache_attention_workspace_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query);
 int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
                           const hifa4_strides* q_strides, const float* s, void* out, void* workspace, size_t workspace_bytes,

@@ -578,7 +578,9 @@ def _strides(t, dev):
 
 def cache_append(cache: PagedCache, k, v, block_table, kv_lens, n_new=None, inv_s=None, tail_slots=None, d_status=None):
     """Smooths and quantizes new keys and values k, v [B,Hkv,n,d] into the cache's pages.  kv_lens [B] counts the new
-    tokens; n_new [B]: how many of the n rows a sequence takes (None: all).  int32 device tensors."""
+    tokens; n_new [B]: how many of the n rows a sequence takes (None: all).  int32 device tensors.
+    Before an append a length may be lowered to a multiple of 64, or inside the last page unless that is full and one append
+    filled it from its first position on (what v_tail holds: include/hifa4.h)."""
     shape = B, Hkv, n, d = k.shape
     dev, dt = _get_device(), k.dtype
     st, sq = cache.struct(_DT[dt], dev), _seqs(block_table, kv_lens, dev, tail_slots)

@@ -142,8 +142,10 @@ cache_append_kernel(const CacheView c, int n, const int* __restrict__ n_new, con
         rows[r * CH + (ch ^ (r >> 4))] = vx[i];
     }
     __syncthreads();
-    if (blockIdx.x == 0) {                                                   // rows of the incomplete page that are new
-        const int t0 = last == p ? lo : 0, t1 = len & 63;
+    if (blockIdx.x == 0) {
+        // New rows that the last page may be continued from: all of an incomplete page; of a page that was begun before and is full now,
+        // all but the last, which any append behind a cut inside the page brings itself (drafted tokens that are taken back).
+        const int used = len - 64 * last, t0 = last == p ? lo : 0, t1 = used < 64 ? used : t0 > 0 ? 63 : 0;
         const uint16_t* vl = v + b * vs.b + h * vs.h + (64ll * last - begin) * vs.t;
         for (int i = tid + t0 * CH; i < t1 * CH; i += 256) tail[i] = __ldg(reinterpret_cast<const uint4*>(vl + i / CH * vs.t) + i % CH);
     }
