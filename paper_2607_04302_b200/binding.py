@@ -544,7 +544,9 @@ def alloc_cache(n_pages, Hkv, d, dtype, device, n_tails) -> PagedCache:
 
 # The kernels run on the current device, so every tensor has to be there (get_device() is -1 on the host).  A step of a short dialogue is
 # bound by host time: the checks of a call share what they look up.
-_get_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+# A torch without CUDA has neither function: the calls refuse there, the import and the size queries work.
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _I32, _FP32 = torch.int32, torch.float32
 
 
