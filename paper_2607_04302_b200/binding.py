@@ -516,7 +516,7 @@ class PagedCache:
         assert nbytes % 74 == 0
         n_tails = 0
         if tail is not None:
-            assert tail.is_cuda and tail.is_contiguous() and tuple(tail.shape[1:]) == (Hkv, PAGE_TOKENS, nbytes // 74)
+            assert tail.get_device() == pages.get_device() and tail.is_contiguous() and tuple(tail.shape[1:]) == (Hkv, PAGE_TOKENS, nbytes // 74)
             n_tails = tail.shape[0]
         # the C descriptors, formed once: a call's host time counts
         make = lambda dt: _Cache(Hkv, nbytes // 74, dt, n_pages, pages.data_ptr(), n_tails, _ptr(tail))

@@ -2,6 +2,10 @@
 import os
 import subprocess
 import sys
+from types import SimpleNamespace
+
+import pytest
+import torch
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -17,3 +21,21 @@ def test_import_and_size_queries_on_a_torch_without_cuda():
             "assert hb.quant_bytes(1, 32, 8, 4096, 128, hb.BF16, hb.Q, hb.CODES) > 0\n")
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
+
+
+def _fake(shape, dtype, device):
+    """What PagedCache asks of a tensor, on a device of this number (-1: the host)."""
+    return SimpleNamespace(shape=torch.Size(shape), dtype=dtype, is_cuda=device >= 0, dim=lambda: len(shape), is_contiguous=lambda: True,
+                           get_device=lambda: device, data_ptr=lambda: 256)
+
+
+@pytest.mark.parametrize("pages_at,tail_at,ok", [(0, 0, True), (1, 1, True), (0, 1, False), (1, 0, False), (0, -1, False), (-1, -1, False)])
+def test_pages_and_tails_are_on_one_device(pages_at, tail_at, ok):
+    """A kernel takes both as pointers of its own device."""
+    from paper_2607_04302_b200 import binding as hb
+    pages, tail = _fake((4, 2, 74 * 64), torch.uint8, pages_at), _fake((3, 2, 64, 64), torch.float16, tail_at)
+    if ok:
+        hb.PagedCache(pages, tail)
+    else:
+        with pytest.raises(AssertionError):
+            hb.PagedCache(pages, tail)
