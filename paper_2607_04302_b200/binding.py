@@ -597,11 +597,11 @@ def cache_append(cache: PagedCache, k, v, block_table, kv_lens, n_new=None, inv_
 
 def cache_read(cache: PagedCache, block_table, kv_lens, n, start=None, out_dtype=BF16, out=None, d_status=None):
     """The values in the cache: (k, v) [B,Hkv,n,d], token i of row b at position start[b] + i (None: i).  Rows at or behind
-    kv_lens[b] are left as they were (out = (k, v): the caller's tensors)."""
+    kv_lens[b] are left as they were in out = (k, v), the caller's tensors, and are zero in new ones."""
     dev = _get_device()
     st, sq = cache.struct(BF16, dev), _seqs(block_table, kv_lens, dev)
     shape = (sq.B, st.Hkv, n, st.d)
-    k, v = out if out is not None else [cache.pages.new_empty(shape, dtype=_TORCH_DT[out_dtype]) for _ in range(2)]
+    k, v = out if out is not None else [cache.pages.new_zeros(shape, dtype=_TORCH_DT[out_dtype]) for _ in range(2)]
     dt = k.dtype
     assert _ok(k, dt, shape, dev) and _ok(v, dt, shape, dev) and (start is None or _ok(start, _I32, shape[:1], dev))
     rc = lib().hifa4_cache_read(C.byref(st), C.byref(sq), n, _ptr(start), _DT[dt], k.data_ptr(), v.data_ptr(), _status(d_status, dev),
