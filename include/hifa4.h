@@ -355,7 +355,8 @@ int hifa4_attention_fwd_raw(const hifa4_shape* shape, const void* q, const void*
  *
  * hifa4_strides: distance in elements between consecutive batch rows, heads and tokens of a 16-bit tensor whose channels are
  * contiguous; multiples of 8, the tensor 16-byte aligned.  NULL: contiguous [B][H][tokens][d].  Factors (s, inv_s) and the
- * outputs of hifa4_cache_read are 16-byte aligned.
+ * outputs of hifa4_cache_read are 16-byte aligned.  Outputs and workspaces overlap no input and not one another, except where a call
+ * says that they may be the same array.
  * ------------------------------------------------------------------------- */
 enum { HIFA4_PAGE_TOKENS = 64 };
 typedef struct {

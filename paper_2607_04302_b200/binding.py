@@ -555,6 +555,12 @@ def _ok(t, dtype, shape, dev):
     return t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous()
 
 
+def _apart(out, q):
+    """Whether the caller's output (contiguous) and the queries do not overlap: the CTAs of a call read q at different times."""
+    a, b = out.data_ptr(), q.data_ptr()
+    return not (a <= b < a + out.nbytes or (q.is_contiguous() and b <= a < b + q.nbytes))
+
+
 def _seqs(block_table, kv_lens, dev, tail_slots=None) -> _Seqs:
     shape = B, max_pages = block_table.shape
     lens = shape[:1]
@@ -644,7 +650,7 @@ def cache_decode(q, cache: PagedCache, block_table, kv_lens, s=None, out=None, l
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
-        assert _ok(out, out.dtype, q_shape, dev)
+        assert _ok(out, out.dtype, q_shape, dev) and _apart(out, q)
     if q_to_kv is not None:
         q_to_kv = _tuple(q_to_kv)
     if workspace is None:
@@ -678,7 +684,7 @@ def cache_attention(q, cache: PagedCache, block_table, kv_lens, causal, s=None, 
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
-        assert _ok(out, out.dtype, q_shape, dev)
+        assert _ok(out, out.dtype, q_shape, dev) and _apart(out, q)
     if q_to_kv is not None:
         q_to_kv = _tuple(q_to_kv)
     if workspace is None:

@@ -39,3 +39,14 @@ def test_pages_and_tails_are_on_one_device(pages_at, tail_at, ok):
     else:
         with pytest.raises(AssertionError):
             hb.PagedCache(pages, tail)
+
+
+def test_outputs_that_overlap_the_queries_are_told():
+    """A tensor over its own queries, or over a part of them; neighbours and interleaved views are fine."""
+    from paper_2607_04302_b200 import binding as hb
+    buf = torch.zeros(4, 6, 64, dtype=torch.float16)
+    q, other = buf[:2], buf[2:]
+    assert hb._apart(other, q) and hb._apart(q, other) and hb._apart(torch.zeros(2, 6, 64), q)
+    assert not hb._apart(q, q) and not hb._apart(buf[1:3], q) and not hb._apart(q, buf[1:3]) and not hb._apart(buf, other)
+    view = buf[:, 2:4]                                       # heads 2 and 3 of every row
+    assert not hb._apart(buf, view) and hb._apart(torch.zeros(4, 2, 64), view) and hb._apart(buf[0, :2], view)

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from tests import cache_reference as ref
-from tests.test_gpu_cache import DEV, DT, P_BITS, check_attention, hb, ints, make_cache
+from tests.test_gpu_cache import DEV, hb, ints, make_cache
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +23,13 @@ def test_read_without_tensors_of_the_caller(dtype):
             for out, want in zip(got, ref.sequence(cache.pages.cpu(), table[b].cpu(), x, h)):
                 m = max(x - at, 0)
                 assert torch.equal(out[b, h, :m].double().cpu(), want[at:]) and (out[b, h, m:] == 0).all()
+
+
+def test_outputs_over_the_queries_are_refused():
+    cache, table, k, v, s, inv_s = make_cache([100], 2, 64, "fp16")
+    q = torch.randn((1, 4, 64), device=DEV).half()
+    q4 = torch.randn((1, 4, 30, 64), device=DEV).half()
+    for call in (lambda: hb().cache_decode(q, cache, table, ints([100]), out=q),
+                 lambda: hb().cache_attention(q4, cache, table, ints([100]), False, out=q4)):
+        with pytest.raises(AssertionError):
+            call()
