@@ -66,7 +66,7 @@ __device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity, volatil
 
 // Two exponentials to base 2 on the multiply-add pipe, for -126 <= x (less counts as -126) and x < 127: x = n + f with n the nearest
 // integer (by adding 1.5 * 2^23, whose low bits then hold n), 2^f by the polynomial of degree 5 that has the least largest relative
-// error on [-1/2, 1/2] (fitted by reweighted least squares; 2.1e-7 with FP32 coefficients and Horner steps), n added to the exponent.
+// error on [-1/2, 1/2] (fitted by reweighted least squares; 2.15e-7 with FP32 coefficients and Horner steps), n added to the exponent.
 __device__ __forceinline__ void exp2_pair(float& x0, float& x1)
 {
     const uint64_t magic = pack2(12582912.f, 12582912.f), unmagic = pack2(-12582912.f, -12582912.f), minus = pack2(-1.f, -1.f);
