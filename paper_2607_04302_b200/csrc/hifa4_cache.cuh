@@ -114,6 +114,8 @@ cudaError_t launch_cache_read(int d, const CacheView& c, int n, const int* start
 cudaError_t launch_cache_evict(const CacheView& c, const float* weight, int keep, int first, int last, int* table_out,
                                int* lens_out, float* weight_out, int* freed, int* n_freed, cudaStream_t st);
 constexpr int DECODE_CTAS = 148;       // one per SM; part of the workspace's size
+// Whether CTAs c0 to c1 can hold a segment.  What a decode kernel that gave up left unwritten in the workspace is arbitrary.
+__host__ __device__ inline bool segment_recorded(int c0, int c1) { return c0 >= 0 && c0 <= c1 && c1 < DECODE_CTAS; }
 // Rows per block for a problem with `rows` rows per KV head at most.
 int decode_block_rows(int d, int rows);
 size_t decode_first_floats(int d, int block_rows);

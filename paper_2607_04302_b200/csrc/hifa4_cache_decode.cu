@@ -856,7 +856,7 @@ cache_join_kernel(const __grid_constant__ DecodeArgs a)
             const int in = j - a.units.first[kv], head = a.units.head[j], r = in % ROWS;
             const int2 cc = a.seg_ctas[(long long)b * U + kv * a.blocks + in / ROWS];
             float2 ml;
-            if ((unsigned)cc.x > (unsigned)cc.y || cc.y >= DECODE_CTAS) {        // nobody said so: the decode kernel gave up
+            if (!segment_recorded(cc.x, cc.y)) {                     // the decode kernel gave up
                 ml = make_float2(-INFINITY, 0.f);
             } else if (cc.x == cc.y) {
                 ml = a.final_ml[(long long)b * a.Hq + head];
