@@ -350,8 +350,8 @@ int hifa4_attention_fwd_raw(const hifa4_shape* shape, const void* q, const void*
  * sequence (0 allowed), for hifa4_cache_append including the new ones; tail_slots [B]: a sequence's row of v_tail, NULL: its
  * index.  All three are DEVICE arrays, so that captured graphs can be replayed with other contents; a length, page or slot
  * out of range is found on the device: its sequence (a page: its tokens) is left out, and *d_status is set to
- * HIFA4_ERR_INVALID_ARG.  Block tables of different sequences may share pages for reading; no two sequences of one
- * hifa4_cache_append may write the same page or tail.
+ * HIFA4_ERR_INVALID_ARG, unless it holds a code already (that of an expired wait is never lost).  Block tables of different
+ * sequences may share pages for reading; no two sequences of one hifa4_cache_append may write the same page or tail.
  *
  * hifa4_strides: distance in elements between consecutive batch rows, heads and tokens of a 16-bit tensor whose channels are
  * contiguous; multiples of 8, the tensor 16-byte aligned.  NULL: contiguous [B][H][tokens][d].  Factors (s, inv_s) and the

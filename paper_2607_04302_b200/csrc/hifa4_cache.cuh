@@ -34,9 +34,14 @@ struct CacheView {
         const int g = __ldg(table + (long long)b * max_pages + p);
         return g < 0 || g >= n_pages ? -1 : g;
     }
+    // The status word keeps the first code, but an expired wait outweighs a bad length, page or slot.
     __device__ __forceinline__ void invalid() const
     {
-        if (d_status) *d_status = HIFA4_ERR_INVALID_ARG;
+        if (d_status) atomicCAS(d_status, 0, HIFA4_ERR_INVALID_ARG);
+    }
+    __device__ __forceinline__ void timed_out() const
+    {
+        if (d_status) atomicMax(d_status, HIFA4_ERR_TIMEOUT);
     }
 };
 

@@ -179,7 +179,7 @@ cache_attention_kernel(const __grid_constant__ TileArgs a)
 
     auto fail = [&]() {
         abort_flag = 1;
-        if (c.d_status) *c.d_status = HIFA4_ERR_TIMEOUT;
+        c.timed_out();
     };
     bool ok = true;
 

@@ -750,7 +750,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs a)
     }
     if (!ok) {
         gave_up = 1;
-        if (lane == 0 && c.d_status) *c.d_status = HIFA4_ERR_TIMEOUT;
+        if (lane == 0) c.timed_out();
         let_copies_land();
     }
     // ---- pieces that warps share: a row of a segment per warp and turn

@@ -126,3 +126,21 @@ def test_two_captured_graphs_with_one_workspace():
                 graphs[i].replay()
             torch.cuda.synchronize()
             assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+def test_a_bad_page_does_not_hide_an_expired_wait():
+    """Several calls may share a status word that is read at the end: what says that outputs are missing stays in it."""
+    lens = [200, 130]
+    cache, table, k, v, s, inv_s = make_cache(lens, 2, 128, "bf16")
+    bad = table.clone()
+    bad[0, 1] = -7
+    q, kv, wrong = torch.randn((2, 4, 128), device=DEV).bfloat16(), ints(lens), ints([-1, 130])
+    calls = [lambda st: hb().cache_decode(q, cache, bad, kv, d_status=st), lambda st: hb().cache_decode(q, cache, table, wrong, d_status=st),
+             lambda st: hb().cache_attention(q[:, :, None].repeat(1, 1, 40, 1), cache, bad, kv, False, d_status=st),
+             lambda st: hb().cache_read(cache, bad, kv, 200, d_status=st), lambda st: hb().cache_evict(table, wrong, torch.zeros(table.shape, device=DEV), 2, d_status=st),
+             lambda st: hb().cache_append(cache, k[:, :, :1].to(DEV), v[:, :, :1].to(DEV), table, wrong, d_status=st)]
+    for before, after in ((0, 1), (6, 6), (6 + 16 * 7, 6 + 16 * 7)):
+        for call in calls:
+            status = torch.full((1,), before, dtype=torch.int32, device=DEV)
+            call(status)
+            assert status.item() == after
