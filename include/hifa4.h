@@ -430,6 +430,15 @@ int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, cons
                           const hifa4_strides* q_strides, const float* s, void* out, void* workspace, size_t workspace_bytes,
                           int* d_status, void* stream);
 
+/* Self-test of the failure path of the two calls' device waits, as hifa4_selftest_wait_timeout: the kernel that hifa4_cache_attention
+ * would take (with page_weight_out: hifa4_cache_decode), in an instantiation whose first CTA's loader leaves a page out (the second
+ * page of its first consumer warp; the third page of a CTA of the kernel on tcgen05) and whose wait for that page ends after 2^6 polls.
+ * *d_status (required, zero on entry) becomes HIFA4_ERR_TIMEOUT; what depends on that CTA is not written or undefined, all else is as
+ * in the ordinary call.  Built for BF16, d = 128 and, of the decode kernel, up to 8 query rows per KV head; q is contiguous. */
+int hifa4_selftest_cache_wait_timeout(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
+                                      void* out, float* page_weight_out, void* workspace, size_t workspace_bytes, int* d_status,
+                                      void* stream);
+
 /* Eviction by accumulated attention weight, whole pages (single tokens would break V's groups).  A sequence of more than
  * keep_pages pages keeps its first keep_first, its last keep_last (>= 1: the incomplete page stays) and, of those between, the
  * keep_pages - keep_first - keep_last with the largest page_weight (equal weights: the lower index; a NaN counts as less than

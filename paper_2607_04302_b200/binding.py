@@ -159,6 +159,8 @@ def lib():
         L.hifa4_cache_attention_workspace_bytes.argtypes = [P(_Cache), I, I, P(_CacheQuery)]
         L.hifa4_cache_attention.restype = I
         L.hifa4_cache_attention.argtypes = [P(_Cache), P(_Seqs), P(_CacheQuery), V, P(_Strides), V, V, V, C.c_size_t, V, V]
+        L.hifa4_selftest_cache_wait_timeout.restype = I
+        L.hifa4_selftest_cache_wait_timeout.argtypes = [P(_Cache), P(_Seqs), P(_CacheQuery), V, V, V, V, C.c_size_t, V, V]
         L.hifa4_cache_evict.restype = I
         L.hifa4_cache_evict.argtypes = [P(_Seqs), V, I, I, I, V, V, V, V, V, V, V]
         _lib = L
@@ -174,7 +176,7 @@ EXPORTS = ("hifa4_status_string", "hifa4_get_counters", "hifa4_smooth_calibrate"
            "hifa4_attention_fwd_qraw", "hifa4_f8qk_workspace_bytes", "hifa4_attention_fwd_f8qk",
            "hifa4_selftest_wait_timeout", "hifa4_cache_page_bytes", "hifa4_cache_append", "hifa4_cache_read",
            "hifa4_cache_decode_workspace_bytes", "hifa4_cache_decode", "hifa4_cache_attention_workspace_bytes",
-           "hifa4_cache_attention", "hifa4_cache_evict")
+           "hifa4_cache_attention", "hifa4_cache_evict", "hifa4_selftest_cache_wait_timeout")
 
 
 def status_string(status: int) -> str:
@@ -698,6 +700,23 @@ def cache_attention(q, cache: PagedCache, block_table, kv_lens, causal, s=None, 
                                      _status(d_status, dev), _raw_stream(dev))
     if rc:
         _check(rc, "hifa4_cache_attention")
+    return out
+
+
+def selftest_cache_wait_timeout(q, cache: PagedCache, block_table, kv_lens, d_status, out, workspace, page_weight_out=None):
+    """Launches the self-test instantiation of the kernel that cache_attention (q [B,Hq,N,d]) or cache_decode (q [B,Hq,d]) would
+    take, in which a wait for a page runs out (see include/hifa4.h); q, out and workspace as for those calls.  d_status holds
+    HIFA4_ERR_TIMEOUT afterwards."""
+    q_shape, shape = q.shape, block_table.shape
+    dev, N = _get_device(), q_shape[2] if q.dim() == 4 else 1
+    st, sq = cache.struct(_DT[q.dtype], dev), _seqs(block_table, kv_lens, dev)
+    assert q.is_contiguous() and q.get_device() == dev and q_shape[-1] == st.d and q_shape[0] == sq.B
+    assert _ok(out, out.dtype, q_shape, dev) and _apart(out, q) and workspace.get_device() == dev
+    assert page_weight_out is None or _ok(page_weight_out, _FP32, shape, dev)
+    rc = lib().hifa4_selftest_cache_wait_timeout(C.byref(st), C.byref(sq), C.byref(_CacheQuery(q_shape[1], None, N, 0, _DT[out.dtype], 0.0)),
+                                                 q.data_ptr(), out.data_ptr(), _ptr(page_weight_out), workspace.data_ptr(), workspace.nbytes,
+                                                 _status(d_status, dev), _raw_stream(dev))
+    _check(rc, "hifa4_selftest_cache_wait_timeout")
     return out
 
 

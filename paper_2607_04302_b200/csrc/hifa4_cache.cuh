@@ -125,9 +125,11 @@ __host__ __device__ inline bool segment_recorded(int c0, int c1) { return c0 >= 
 int decode_block_rows(int d, int rows);
 size_t decode_first_floats(int d, int block_rows);
 cudaError_t launch_cache_decode(int dtype, int d, int block_rows, const DecodeArgs& a, cudaStream_t st);
+cudaError_t launch_cache_decode_selftest(const DecodeArgs& a, cudaStream_t st);          // BF16, d = 128, 8 rows
 
 // Query rows that a CTA of the tensor-memory kernel takes.
 int attention_tile_rows(int dtype, int d);
 cudaError_t launch_cache_attention(int dtype, int d, const TileArgs& a, cudaStream_t st);
+cudaError_t launch_cache_attention_selftest(const TileArgs& a, cudaStream_t st);         // BF16, d = 128
 
 }  // namespace hifa4

@@ -141,7 +141,7 @@ int check_call(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cac
 
 int run_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const CacheUnits& units, int rows,
                Strides qs, const void* q, const float* s, void* out, float* lse, const float* weight, float* weight_out,
-               void* workspace, size_t workspace_bytes, int* d_status, void* stream)
+               void* workspace, size_t workspace_bytes, int* d_status, void* stream, bool selftest = false)
 {
     const DecodeLayout lay(cache, seqs->B, seqs->max_pages, query, rows, weight_out != nullptr);
     if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;
@@ -167,8 +167,9 @@ int run_decode(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cac
     a.seg_ctas = weight_out ? (int2*)(ws + lay.seg_ctas) : nullptr;
     a.final_ml = weight_out ? (float2*)(ws + lay.final_ml) : nullptr;
     a.page_ml = weight_out ? (float2*)(ws + lay.page_ml) : nullptr;
-    return launch_cache_decode(cache->in_dtype, cache->d, lay.block_rows, a, (cudaStream_t)stream) == cudaSuccess ? HIFA4_OK
-                                                                                                                  : HIFA4_ERR_CUDA;
+    const cudaError_t e = selftest ? launch_cache_decode_selftest(a, (cudaStream_t)stream)
+                                   : launch_cache_decode(cache->in_dtype, cache->d, lay.block_rows, a, (cudaStream_t)stream);
+    return e == cudaSuccess ? HIFA4_OK : HIFA4_ERR_CUDA;
 }
 
 // The tensor-memory kernel's grid and workspace.  A CTA has an SM to itself; blocks come in waves, and a last wave that does not
@@ -212,6 +213,30 @@ struct TileLayout {
 // 1500, 8 rows 10.4 and 13.6, 16 13.0 and 13.6.  d = 256, whose decode kernel takes 8 rows at a time: 8 of 4096, 8 rows 37 and 55, 16
 // 57 and 56.  (One sequence of 300 takes 11 and 10 us at 2 to 8 rows; the host does not know lengths.)
 bool tile_kernel_faster(int d, int rows) { return rows > (d == 256 ? 8 : 16); }
+
+int run_tiles(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const CacheUnits& units, int rows,
+              Strides qs, const void* q, const float* s, void* out, void* workspace, size_t workspace_bytes, int* d_status, void* stream,
+              bool selftest = false)
+{
+    const TileLayout lay(cache, seqs->B, seqs->max_pages, rows);
+    if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;
+    if (lay.blocks * 32 * lay.splits > 0x7FFFFFFFll) return HIFA4_ERR_UNSUPPORTED;
+    const int rc = check_arch();
+    if (rc) return rc;
+    TileArgs a;
+    std::memset(&a, 0, sizeof(a));
+    common_args(a, cache, seqs, query, q, s, out, d_status);
+    a.units = units;
+    a.qs = qs;
+    a.items = (int)lay.items;
+    a.full = (int)lay.full;
+    a.splits = lay.splits;
+    a.part_o = (float*)workspace;
+    a.part_ml = (float2*)((char*)workspace + lay.part_ml);
+    const cudaError_t e = selftest ? launch_cache_attention_selftest(a, (cudaStream_t)stream)
+                                   : launch_cache_attention(cache->in_dtype, cache->d, a, (cudaStream_t)stream);
+    return e == cudaSuccess ? HIFA4_OK : HIFA4_ERR_CUDA;
+}
 
 // Workspace of a call; 0 where it is not built.
 size_t attend_bytes(const hifa4_cache* cache, int B, int max_pages, const hifa4_cache_query* query, bool weight, bool many)
@@ -304,21 +329,27 @@ int hifa4_cache_attention(const hifa4_cache* cache, const hifa4_seqs* seqs, cons
     if (rc) return rc;
     if (!tile_kernel_faster(cache->d, rows))
         return run_decode(cache, seqs, query, units, rows, qs, q, s, out, nullptr, nullptr, nullptr, workspace, workspace_bytes, d_status, stream);
-    const TileLayout lay(cache, seqs->B, seqs->max_pages, rows);
-    if (!workspace || workspace_bytes < lay.total || ((uintptr_t)workspace & 255)) return HIFA4_ERR_WORKSPACE;
-    if (lay.blocks * 32 * lay.splits > 0x7FFFFFFFll) return HIFA4_ERR_UNSUPPORTED;
-    if ((rc = check_arch())) return rc;
-    TileArgs a;
-    std::memset(&a, 0, sizeof(a));
-    common_args(a, cache, seqs, query, q, s, out, d_status);
-    a.units = units;
-    a.qs = qs;
-    a.items = (int)lay.items;
-    a.full = (int)lay.full;
-    a.splits = lay.splits;
-    a.part_o = (float*)workspace;
-    a.part_ml = (float2*)((char*)workspace + lay.part_ml);
-    return launch_cache_attention(cache->in_dtype, cache->d, a, (cudaStream_t)stream) == cudaSuccess ? HIFA4_OK : HIFA4_ERR_CUDA;
+    return run_tiles(cache, seqs, query, units, rows, qs, q, s, out, workspace, workspace_bytes, d_status, stream);
+}
+
+int hifa4_selftest_cache_wait_timeout(const hifa4_cache* cache, const hifa4_seqs* seqs, const hifa4_cache_query* query, const void* q,
+                                      void* out, float* page_weight_out, void* workspace, size_t workspace_bytes, int* d_status,
+                                      void* stream)
+{
+    if (!d_status) return HIFA4_ERR_INVALID_ARG;
+    CacheUnits units;
+    int rows;
+    Strides qs;
+    const int rc = check_call(cache, seqs, query, q, nullptr, nullptr, out, &units, &rows, &qs);
+    if (rc) return rc;
+    if (cache->in_dtype != HIFA4_BF16 || cache->d != 128) return HIFA4_ERR_UNSUPPORTED;
+    if (tile_kernel_faster(cache->d, rows)) {
+        if (page_weight_out) return HIFA4_ERR_UNSUPPORTED;
+        return run_tiles(cache, seqs, query, units, rows, qs, q, nullptr, out, workspace, workspace_bytes, d_status, stream, true);
+    }
+    if (decode_block_rows(cache->d, rows) != 8 || (page_weight_out && query->N != 1)) return HIFA4_ERR_UNSUPPORTED;
+    return run_decode(cache, seqs, query, units, rows, qs, q, nullptr, out, nullptr, nullptr, page_weight_out, workspace, workspace_bytes,
+                      d_status, stream, true);
 }
 
 int hifa4_cache_evict(const hifa4_seqs* seqs, const float* page_weight, int keep_pages, int keep_first, int keep_last,
