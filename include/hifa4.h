@@ -357,6 +357,11 @@ int hifa4_attention_fwd_raw(const hifa4_shape* shape, const void* q, const void*
  * contiguous; multiples of 8, the tensor 16-byte aligned.  NULL: contiguous [B][H][tokens][d].  Factors (s, inv_s) and the
  * outputs of hifa4_cache_read are 16-byte aligned.  Outputs and workspaces overlap no input and not one another, except where a call
  * says that they may be the same array.
+ *
+ * Sizes: B * Hkv up to 65535, max_pages up to 2^24, N up to 2^20, (2 max_pages + 1) * B * Hkv * (blocks of 8 or 16 query rows per KV head)
+ * up to 2 * 10^9 for attention of few query rows; beyond them HIFA4_ERR_UNSUPPORTED.  Kernels read a table only as far as its sequences reach,
+ * but its width is all that the host knows of their lengths: it sets the workspaces (page weights: 8 B Hq max_pages bytes) and how
+ * hifa4_cache_attention shares its work out.
  * ------------------------------------------------------------------------- */
 enum { HIFA4_PAGE_TOKENS = 64 };
 typedef struct {
